@@ -7,6 +7,7 @@
 // nibble with the 3-bit extended mantissa, and each lane stores one dword of nibbles.  Scale and index bytes of
 // four neighbouring blocks are gathered into one lane and stored as dwords.
 #include "mxp_common.h"
+#include "mxp_encode.h"
 #include "mxp_prepack_body.h"
 #include <type_traits>
 
@@ -17,140 +18,6 @@ using namespace mxp;
 typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-
-template <int CTRL>
-__device__ __forceinline__ uint32_t dpp_mov(uint32_t v) {
-  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, true);
-}
-constexpr int kQuadSwap1 = 0xB1;  // quad_perm [1,0,3,2]
-constexpr int kQuadSwap2 = 0x4E;  // quad_perm [2,3,0,1]
-constexpr int kRowShr4 = 0x114;
-constexpr int kRowShr8 = 0x118;
-
-__device__ __forceinline__ uint32_t umax(uint32_t a, uint32_t b) { return a > b ? a : b; }
-__device__ __forceinline__ uint32_t umin(uint32_t a, uint32_t b) { return a < b ? a : b; }
-
-// 3-bit BM mantissa from the 23-bit fraction of the block maximum: round to nearest even on bit 20, and a carry
-// out of the field saturates (the shared scale is never altered, Sec. 4.1).
-__device__ __forceinline__ uint32_t bm_mantissa(uint32_t frac23) {
-  uint32_t m = (frac23 + 0x7FFFFu + ((frac23 >> 20) & 1u)) >> 20;
-  return umin(m, 7u);
-}
-
-// One group = 8 consecutive elements of one block, held by one lane.  `part` = which quarter of the block.
-// Returns the packed dword of 8 nibbles; scale byte and index byte are returned in all four lanes of the quad.
-// MODE: 0 = MXFP4, 1 = MXFP4+, 2 = MXFP4++ (Sec. 4.3: the NBMs are scaled by 2^(shared_exp - delta), where
-// shared_exp - delta = CLIP(largest NBM exponent - e_max + 1, {shared_exp - 7, shared_exp}), and delta goes into bits
-// 7:5 of the index byte; delta is also kept <= scale byte - 1 so that the NBM scale stays an E8M0 number).
-template <bool BF16, int MODE>
-__device__ __forceinline__ uint32_t encode_group(const uint32_t (&w)[8], int part, uint32_t& sbyte, uint32_t& idx) {
-  constexpr bool PLUS = MODE >= 1, PP = MODE == 2;
-  uint32_t amax32;  // magnitude bits of the block maximum, as an fp32 pattern
-  uint32_t a2 = 0;  // (PP) magnitude bits of the largest element other than the BM
-  if (BF16) {
-    // key = magnitude(15 bit) << 16 | (31 - position): one unsigned max gives the maximum and, among equal
-    // magnitudes, the lowest position.
-    uint32_t k = 0;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      uint32_t m = w[j] & 0x7FFF7FFFu;
-      uint32_t klo = (m << 16) | (uint32_t)(7 - 2 * j);
-      uint32_t khi = (m & 0xFFFF0000u) | (uint32_t)(6 - 2 * j);
-      k = umax(k, umax(klo, khi));
-    }
-    k += (uint32_t)(3 - part) * 8u;
-    k = umax(k, dpp_mov<kQuadSwap1>(k));
-    k = umax(k, dpp_mov<kQuadSwap2>(k));
-    amax32 = k & 0xFFFF0000u;
-    idx = 31u - (k & 31u);
-    if (PP) {
-      // keys are unique (the position is part of them): the lane whose best key won leaves that element out
-      uint32_t k2 = 0;
-      const uint32_t off = (uint32_t)(3 - part) * 8u;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const uint32_t m = w[j] & 0x7FFF7FFFu;
-        const uint32_t klo = ((m << 16) | (uint32_t)(7 - 2 * j)) + off;
-        const uint32_t khi = ((m & 0xFFFF0000u) | (uint32_t)(6 - 2 * j)) + off;
-        k2 = umax(k2, klo == k ? 0u : klo);
-        k2 = umax(k2, khi == k ? 0u : khi);
-      }
-      k2 = umax(k2, dpp_mov<kQuadSwap1>(k2));
-      k2 = umax(k2, dpp_mov<kQuadSwap2>(k2));
-      a2 = k2 & 0xFFFF0000u;
-    }
-  } else {
-    uint32_t a[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) a[i] = w[i] & 0x7FFFFFFFu;
-    uint32_t mx = a[0];
-#pragma unroll
-    for (int i = 1; i < 8; ++i) mx = umax(mx, a[i]);
-    mx = umax(mx, dpp_mov<kQuadSwap1>(mx));
-    mx = umax(mx, dpp_mov<kQuadSwap2>(mx));
-    uint32_t p = 32u;
-#pragma unroll
-    for (int i = 7; i >= 0; --i) p = (a[i] == mx) ? (uint32_t)(part * 8 + i) : p;
-    p = umin(p, dpp_mov<kQuadSwap1>(p));
-    p = umin(p, dpp_mov<kQuadSwap2>(p));
-    amax32 = mx;
-    idx = p;
-    if (PP) {
-      uint32_t m2 = 0;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) m2 = umax(m2, (uint32_t)(part * 8 + i) == p ? 0u : a[i]);
-      m2 = umax(m2, dpp_mov<kQuadSwap1>(m2));
-      m2 = umax(m2, dpp_mov<kQuadSwap2>(m2));
-      a2 = m2;
-    }
-  }
-  const uint32_t E = amax32 >> 23;                     // biased exponent of the BM = floor(log2) + 127
-  const bool flush = E <= 2u;                          // floor(log2 BM) <= -127 + e_max      (Sec. 4.1)
-  const bool nonfinite = E == 255u;
-  uint32_t delta = 0;
-  if (PP) {
-    const uint32_t sb = E - 2u, E2 = a2 >> 23;                       // biased: BM scale; exponent of the largest NBM
-    const uint32_t lo = sb > 7u ? sb - 7u : 0u;                      // (flushed blocks are reset below)
-    uint32_t nb = E2 == 0u ? lo : umin(umax(E2 - 1u, lo), sb);       // biased shared_exp_new = E2 - 127 - e_max + 1 + 127
-    nb = umax(nb, 1u);
-    delta = sb - nb;
-  }
-  // X = 2^shared_exp, shared_exp = floor(log2 BM) - e_max (Eq. 1); the NBMs of MXFP4++ use 2^(shared_exp - delta)
-  const float scale = __uint_as_float((E - 2u - delta) << 23);
-  uint32_t packed = 0;
-  if (BF16) {
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      union { uint32_t u; v2bf v; } c;
-      c.u = w[j];
-      if (j == 0) packed = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(packed, c.v, scale, 0);
-      if (j == 1) packed = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(packed, c.v, scale, 1);
-      if (j == 2) packed = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(packed, c.v, scale, 2);
-      if (j == 3) packed = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(packed, c.v, scale, 3);
-    }
-  } else {
-    packed = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(packed, __uint_as_float(w[0]), __uint_as_float(w[1]), scale, 0);
-    packed = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(packed, __uint_as_float(w[2]), __uint_as_float(w[3]), scale, 1);
-    packed = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(packed, __uint_as_float(w[4]), __uint_as_float(w[5]), scale, 2);
-    packed = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(packed, __uint_as_float(w[6]), __uint_as_float(w[7]), scale, 3);
-  }
-  if (PLUS) {
-    // BM nibble = sign | m2 m1 m0 ; the sign is already in the converted nibble.
-    const uint32_t m3 = bm_mantissa(amax32 & 0x7FFFFFu);
-    const uint32_t sh = (idx & 7u) * 4u;
-    const uint32_t nib = ((packed >> sh) & 8u) | m3;
-    const uint32_t repl = (packed & ~(0xFu << sh)) | (nib << sh);
-    packed = ((idx >> 3) == (uint32_t)part) ? repl : packed;
-  }
-  sbyte = E - 2u;
-  if (PP) idx |= delta << 5;
-  if (flush || nonfinite) {
-    packed = 0;
-    idx = 0;
-    sbyte = nonfinite ? 255u : 0u;
-  }
-  return packed;
-}
 
 template <bool BF16>
 __device__ __forceinline__ void load_group(const void* __restrict__ src, int64_t q, int64_t nbk, int64_t ld, bool dense,

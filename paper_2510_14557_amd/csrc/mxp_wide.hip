@@ -13,80 +13,15 @@
 // results could leave the fp32 normal range, through integer code on the fields of the fp32 pattern (nothing there
 // depends on the float mode).
 #include "mxp_common.h"
+#include "mxp_encode.h"
 
 namespace {
 
 using namespace mxp;
 
+typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
-typedef short v2s __attribute__((ext_vector_type(2)));
-#ifndef MXP_WIDE_HW_FP8
-#define MXP_WIDE_HW_FP8 1
-#endif
-
-template <int CTRL>
-__device__ __forceinline__ uint32_t dpp_mov(uint32_t v) {
-  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, true);
-}
-constexpr int kQuadSwap1 = 0xB1;   // quad_perm [1,0,3,2]
-constexpr int kQuadSwap2 = 0x4E;   // quad_perm [2,3,0,1]
-constexpr int kQuadFromEven = 0xA0;  // quad_perm [0,0,2,2]: odd lanes read their left neighbour
-
-__device__ __forceinline__ uint32_t umax(uint32_t a, uint32_t b) { return a > b ? a : b; }
-__device__ __forceinline__ uint32_t umin(uint32_t a, uint32_t b) { return a < b ? a : b; }
-
-template <int BITS>
-struct Elem;
-template <>
-struct Elem<6> {   // E2M3
-  static constexpr int MB = 3, BIAS = 1, EMAX = 2;
-  static constexpr uint32_t MAXCODE = 0x1Fu;   // 7.5
-};
-template <>
-struct Elem<8> {   // E4M3 (OCP): S.1111.111 is NaN, the largest number is S.1111.110 = 448
-  static constexpr int MB = 3, BIAS = 7, EMAX = 8;
-  static constexpr uint32_t MAXCODE = 0x7Eu;
-};
-
-// Round-to-nearest-even of sig >> shift, 1 <= shift <= 31.
-__device__ __forceinline__ uint32_t rne_shift(uint32_t sig, uint32_t shift) {
-  const uint32_t t = sig >> shift, rem = sig & ((1u << shift) - 1u), half = 1u << (shift - 1u);
-  return t + ((rem > half || (rem == half && (t & 1u))) ? 1u : 0u);
-}
-
-// Magnitude code of an ordinary element: a = fp32 magnitude bits of x, the block scale is 2^(sbyte - 127).
-// exponent/mantissa fields are produced as one integer, so a mantissa carry moves into the exponent by itself and
-// the subnormal range (field 0) needs no case of its own beyond its larger shift.
-template <int BITS>
-__device__ __forceinline__ uint32_t elem_code(uint32_t a, int sbyte) {
-  using F = Elem<BITS>;
-  if (a == 0u) return 0u;
-  int ea = (int)(a >> 23);
-  uint32_t sig = a & 0x7FFFFFu;
-  if (ea == 0) {                       // fp32 subnormal input: normalise so that bit 23 is the leading one
-    const int lz = __builtin_clz(sig) - 8;
-    sig <<= lz;
-    ea = 1 - lz;
-  } else {
-    sig |= 0x800000u;
-  }
-  const int t = ea - sbyte + F::BIAS;  // exponent field the scaled value would have as a normal number
-  const int eff = t > 1 ? t : 1;
-  int shift = (23 - F::MB) + (eff - t);
-  shift = shift > 31 ? 31 : shift;     // sig < 2^24: everything beyond 25 rounds to zero anyway
-  const uint32_t code = ((uint32_t)(eff - 1) << F::MB) + rne_shift(sig, (uint32_t)shift);
-  return umin(code, F::MAXCODE);
-}
-
-// BM mantissa of a + format: FB = BITS - 1 fraction bits at exponent e_max; a carry out of the field saturates (the
-// shared scale is never altered, Sec. 4.1).  The BM of a block that is not flushed is a normal fp32 number.
-template <int BITS>
-__device__ __forceinline__ uint32_t bm_code(uint32_t a) {
-  constexpr int FB = BITS - 1;
-  return umin(rne_shift(a & 0x7FFFFFu, 23 - FB), (1u << FB) - 1u);
-}
 
 // fp32 pattern of (-1)^sign * M * 2^p for M < 2^24, built from integer fields (exact whenever p >= -149; results
 // below the normal range are the value in units of 2^-149).
@@ -122,7 +57,6 @@ template <bool BF16, int BITS, bool PLUS, bool DENSE>
 __global__ void __launch_bounds__(256) quantize_wide_kernel(const void* __restrict__ src, int64_t nbk, int64_t ld, int64_t nq,
                                                             uint8_t* __restrict__ elems, uint8_t* __restrict__ scales,
                                                             uint8_t* __restrict__ bm_idx) {
-  using F = Elem<BITS>;
   const uint32_t part = threadIdx.x & 3u;
   const int64_t stride = (int64_t)gridDim.x * 256;
   for (int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x; (q & ~(int64_t)3) < nq; q += stride) {
@@ -156,73 +90,8 @@ __global__ void __launch_bounds__(256) quantize_wide_kernel(const void* __restri
         sg[i] = w[i] >> 31;
       }
     }
-    uint32_t mx = a[0];
-#pragma unroll
-    for (int i = 1; i < 8; ++i) mx = umax(mx, a[i]);
-    mx = umax(mx, dpp_mov<kQuadSwap1>(mx));
-    mx = umax(mx, dpp_mov<kQuadSwap2>(mx));
-    uint32_t pos = 32u;                             // lowest position holding the maximum
-#pragma unroll
-    for (int i = 7; i >= 0; --i) pos = (a[i] == mx) ? part * 8u + (uint32_t)i : pos;
-    pos = umin(pos, dpp_mov<kQuadSwap1>(pos));
-    pos = umin(pos, dpp_mov<kQuadSwap2>(pos));
-    const uint32_t E = mx >> 23;
-    const bool flush = E <= (uint32_t)F::EMAX, nonfinite = E == 255u;
-    const int sbyte = (int)E - F::EMAX;             // Eq. 1
-    uint32_t lo = 0, hi = 0;                        // this lane's code bits: 48 (lo, hi[15:0]) or 64
-    if (BITS == 8 && MXP_WIDE_HW_FP8) {
-      // E4M3 elements: the CDNA4 pack-convert (x / X, round to nearest even, sign kept), two per instruction; the BM
-      // byte of a + format is replaced afterwards
-      const float X = __uint_as_float((uint32_t)(sbyte > 0 ? sbyte : 1) << 23);
-      v2s plo = {0, 0}, phi = {0, 0};
-      if (BF16) {
-        union { uint32_t u; v2bf v; } c0, c1, c2, c3;
-        c0.u = raw[0]; c1.u = raw[1]; c2.u = raw[2]; c3.u = raw[3];
-        plo = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(plo, c0.v, X, false);
-        plo = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(plo, c1.v, X, true);
-        phi = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(phi, c2.v, X, false);
-        phi = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(phi, c3.v, X, true);
-      } else {
-        plo = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(plo, __uint_as_float(raw[0]), __uint_as_float(raw[1]), X, false);
-        plo = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(plo, __uint_as_float(raw[2]), __uint_as_float(raw[3]), X, true);
-        phi = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(phi, __uint_as_float(raw[4]), __uint_as_float(raw[5]), X, false);
-        phi = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(phi, __uint_as_float(raw[6]), __uint_as_float(raw[7]), X, true);
-      }
-      union { v2s v; uint32_t u; } ul, uh;
-      ul.v = plo;
-      uh.v = phi;
-      // the instruction answers magnitudes that round above 448 with the NaN code S.1111.111; the format saturates:
-      // clear bit 0 of every byte whose low seven bits are all ones
-      lo = ul.u & ~((((ul.u & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u) >> 7);
-      hi = uh.u & ~((((uh.u & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u) >> 7);
-      if (PLUS && (pos >> 3) == part) {
-        const uint32_t i = pos & 7u, sh = (i & 3u) * 8u;
-        uint32_t ai = 0, si = 0;
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          ai = i == (uint32_t)k ? a[k] : ai;
-          si = i == (uint32_t)k ? sg[k] : si;
-        }
-        const uint32_t code = bm_code<8>(ai) | (si << 7);
-        if (i < 4u) lo = (lo & ~(0xFFu << sh)) | (code << sh);
-        else hi = (hi & ~(0xFFu << sh)) | (code << sh);
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        uint32_t c = (PLUS && pos == part * 8u + (uint32_t)i) ? bm_code<BITS>(a[i]) : elem_code<BITS>(a[i], sbyte);
-        c |= sg[i] << (BITS - 1);
-        const int b = i * BITS;                     // bit position inside the lane's string
-        if (b < 32) lo |= c << b;
-        if (b + BITS > 32) hi |= (b >= 32) ? (c << (b - 32)) : (c >> (32 - b));
-      }
-    }
-    uint32_t sb = (uint32_t)sbyte, idx = pos;
-    if (flush || nonfinite) {
-      lo = hi = 0;
-      idx = 0;
-      sb = nonfinite ? 255u : 0u;
-    }
+    uint32_t lo, hi, sb, idx;
+    encode_wide_group<BF16, BITS, PLUS>(raw, a, sg, part, lo, hi, sb, idx);
     if (BITS == 8) {
       if (q < nq) *reinterpret_cast<u32x2*>(elems + g * 32 + part * 8) = u32x2{lo, hi};
     } else {
