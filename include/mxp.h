@@ -106,6 +106,18 @@ int mxp_quantize_t(const void* src, int src_dtype, int64_t rows, int64_t K, int6
 int mxp_quantize_gather(const void* src, int src_dtype, int64_t rows, int64_t K, int64_t n_src, int64_t ld_src,
                         const int32_t* perm, int fmt, uint8_t* elems, uint8_t* scales, uint8_t* bm_idx, void* stream);
 
+/* Root-mean-square norm with the residual's addition, converted in the same pass: what stands in front of a product whose
+ * activations are quantized at run time (Sec. 7.1).  Per row, in fp32:
+ *     h = x + residual, rounded to x's type;   y = h * 1 / sqrt(sum(h^2) / K + eps) * weight;   y -> block format fmt
+ * with any of the seven formats and the block rule of mxp_quantize (y is not rounded before the conversion).  x, residual (NULL:
+ * h = x) and h (NULL: not kept) share x_dtype, each with its row stride; h may be x or residual itself (same pointer and row
+ * stride) and must not overlap them otherwise.  weight[K] has its own dtype.  elems / scales / bm_idx as for mxp_quantize.  The sum of
+ * squares is an fp32 number: a row whose sum overflows, or that holds a NaN or Inf, comes out as IEEE arithmetic has it (its NaN
+ * blocks with scale byte 255).  eps is finite and not negative (else MXP_ERR_SHAPE), K at most 2^21 (else MXP_ERR_UNSUPPORTED). */
+int mxp_rmsnorm_quantize(const void* x, const void* residual, int x_dtype, int64_t rows, int64_t K, int64_t ld_x, int64_t ld_residual,
+                         const void* weight, int w_dtype, float eps, void* h, int64_t ld_h, int fmt, uint8_t* elems, uint8_t* scales,
+                         uint8_t* bm_idx, void* stream);
+
 /* De-conversion (Eq. 2): dst[r][k] = (-1)^s * 2^shared_exp * E, with E = 2^e_max * 1.mmm for the BM position of an
  * MXFP4+ block and the E2M1 value otherwise.  Scale byte 0 gives zeros (tested before the BM branch), 255 gives NaN.
  * For MXFP4++ the non-BM elements use 2^(shared_exp - delta), delta = index byte bits 7:5 (MXFP4+ ignores those bits).
@@ -344,6 +356,54 @@ size_t mxp_gemm_w4a16_workspace_bytes(int64_t M, int64_t N, int64_t K, int fmtW)
 int mxp_gemm_w4a16_ws(int64_t M, int64_t N, int64_t K, const void* A, int a_dtype, int64_t lda,
                       const uint8_t* W_elems, const uint8_t* W_scales, const uint8_t* W_idx, int fmtW,
                       void* D, int d_dtype, int64_t ldd, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---- A paged key-value cache in four-bit blocks, and attention over it -------------------------------------------------
+ * The keys and values of past tokens are operands of a product like any other and are quantized like them (the paper's
+ * direct-cast setting includes the KV cache).  The cache is one device array of n_pages pages of page_tokens tokens
+ * (16, 32, 64, 128 or 256) in MXFP4, MXFP4+ or MXFP4++, head_dim 64, 128 or 256; other formats, pages and heads return
+ * MXP_ERR_UNSUPPORTED.  Per page and key-value head it holds a record of keys and, behind it, one of values; a record is
+ *     elems [page_tokens][head_dim / 2] | scales [page_tokens][head_dim / 32] | bm_idx [page_tokens][head_dim / 32]
+ * in canonical encoding with the blocks along the head (MXFP4: no bm_idx): records lie [page][kv_head][keys, values].
+ * mxp_cache_bytes: the size of the array (0 for arguments that are refused).  It needs no initialisation: only slots that were
+ * written are ever used.  A token's slot is page * page_tokens + its place in the page. */
+size_t mxp_cache_bytes(int64_t n_pages, int64_t page_tokens, int64_t kv_heads, int64_t head_dim, int fmt);
+
+/* Quantizes K and V, [tokens][kv_heads][head_dim] (the heads of a token without gaps, tokens ld_k / ld_v elements apart, as in a
+ * slice of a joint projection), into the slots of their tokens: bytes as mxp_quantize writes them.  slots: device array; a slot
+ * outside the cache (-1 for the padding of a batch, say) means that the token is not kept.  The slots that are kept must be
+ * distinct: one given twice holds a mixture of both tokens afterwards. */
+int mxp_cache_write(const void* K, const void* V, int src_dtype, int64_t tokens, int64_t ld_k, int64_t ld_v, const int64_t* slots,
+                    void* cache, int64_t n_pages, int64_t page_tokens, int64_t kv_heads, int64_t head_dim, int fmt, void* stream);
+
+/* The reverse: K and V rows of the given slots (in any order, a slot more than once if wanted), values as mxp_dequantize gives
+ * them; rows of slots outside the cache are zeros. */
+int mxp_cache_read(const void* cache, int64_t n_pages, int64_t page_tokens, int64_t kv_heads, int64_t head_dim, int fmt,
+                   const int64_t* slots, int64_t tokens, void* K, void* V, int dst_dtype, int64_t ld_k, int64_t ld_v, void* stream);
+
+/* Attention over the cache.  Sequence s has kv_len[s] tokens in the cache; token t lies in page table[s * ld_table + t / page_tokens]
+ * at place t % page_tokens (ld_table: entries per sequence; a longer kv_len counts as ld_table * page_tokens, and at most 2^30).  Its queries are rows
+ * q_start[s] .. q_start[s + 1] - 1 of Q [rows][heads][head_dim] (rows ld_q elements apart; q_start holds n_seq + 1 numbers that do
+ * not fall; NULL: one row per sequence, rows == n_seq).  Rows of Q before the first and behind the last sequence are not read, and
+ * their rows of O and lse left as they are.  Query head j reads key-value head j / (heads / kv_heads).
+ *     O = sum_t p_t v_t,   p = softmax over the visible t of  scale * q . k_t,   lse = log sum_t exp(scale * q . k_t)
+ * causal: query i of n sees token t <= kv_len - n + i (the last query sees all); with window > 0 (causal only) also
+ * t > kv_len - n + i - window.  Not causal: every t < kv_len.  A page number outside [0, n_pages) stands for tokens that nobody sees.
+ * A row that sees nothing gets O = 0 and lse = -infinity.  What an invisible token's slot holds, a NaN block included, has no
+ * influence; a visible NaN block makes the scores (keys) or the 32 outputs (values) it meets NaN.
+ * Q is MXP_BF16 (MXP_F32: MXP_ERR_UNSUPPORTED); keys and values are de-converted by Eq. 2 (exact) inside the kernel and multiplied
+ * on the bf16 MFMA; scores, softmax and sums are fp32.  For fp32 O the weights p enter the second product as two bf16 terms
+ * (to 2^-16 of each), for bf16 O as one (to 2^-8).  Values below 2^-126 may count as zero.  lse [rows][heads] fp32 may be NULL.
+ * kv_len, table and q_start are read on the device only.  max_q and max_kv are the caller's upper bounds on queries and kv_len of a
+ * sequence: they choose launch and splitting, larger sequences are computed all the same, more slowly.
+ * rows * heads is at most 2^30 (else MXP_ERR_UNSUPPORTED).
+ * workspace: mxp_attention_workspace_bytes(...) of the same arguments (may be 0), scratch for the parts of split sequences, free
+ * again after the call's work on `stream`; a smaller one returns MXP_ERR_WORKSPACE. */
+size_t mxp_attention_workspace_bytes(int64_t n_seq, int64_t rows, int64_t max_q, int64_t max_kv, int64_t heads, int64_t kv_heads,
+                                     int64_t head_dim, int64_t window);
+int mxp_attention(const void* Q, int q_dtype, int64_t ld_q, int64_t rows, int64_t heads, const int32_t* q_start, const int32_t* kv_len,
+                  const int32_t* table, int64_t ld_table, int64_t n_seq, int64_t max_q, int64_t max_kv, float scale, int causal,
+                  int64_t window, const void* cache, int64_t n_pages, int64_t page_tokens, int64_t kv_heads, int64_t head_dim, int fmt,
+                  void* O, int o_dtype, int64_t ld_o, float* lse, void* workspace, size_t workspace_bytes, void* stream);
 
 const char* mxp_status_string(int status);
 int mxp_version(void);

@@ -11,6 +11,7 @@ from __future__ import annotations
 import ctypes as C
 import os
 import warnings
+from typing import NamedTuple
 
 import torch
 
@@ -25,7 +26,8 @@ LIB_PATH = os.path.join(_HERE, "libmxp.so")
 
 EXPORTS = ("mxp_quantize", "mxp_quantize_t", "mxp_quantize_gather", "mxp_dequantize", "mxp_image_bytes", "mxp_prepack", "mxp_quantize_image",
            "mxp_image_bytes_e2m1", "mxp_prepack_e2m1", "mxp_image_bytes_e2m1r", "mxp_prepack_e2m1r", "mxp_prepack_e2m1x", "mxp_image_bytes_e4m3", "mxp_prepack_e4m3", "mxp_gemm_workspace_bytes", "mxp_gemm_workspace_bytes_e4m3", "mxp_gemm_workspace_bytes_fmt", "mxp_image_bytes_fp6", "mxp_prepack_fp6", "mxp_quantize_image_fp6", "mxp_prepack_seg", "mxp_prepack_fp8", "mxp_gemm", "mxp_gemm_prepacked", "mxp_gemm_bf16a_workspace_bytes", "mxp_gemm_decode", "mxp_gemm_decode_bf16a",
-           "mxp_gemm_bf16a", "mxp_gemm_w4a16", "mxp_gemm_w4a16_workspace_bytes", "mxp_gemm_w4a16_ws", "mxp_convert_operands", "mxp_gemm_workspace_size", "mxp_gemm_static", "mxp_gemm_static_capacity", "mxp_status_string", "mxp_version")
+           "mxp_gemm_bf16a", "mxp_gemm_w4a16", "mxp_gemm_w4a16_workspace_bytes", "mxp_gemm_w4a16_ws", "mxp_convert_operands", "mxp_gemm_workspace_size", "mxp_gemm_static", "mxp_gemm_static_capacity",
+           "mxp_rmsnorm_quantize", "mxp_cache_bytes", "mxp_cache_write", "mxp_cache_read", "mxp_attention_workspace_bytes", "mxp_attention", "mxp_status_string", "mxp_version")
 
 _lib = None
 _fast = None                                               # _mxp_binding or _NoNative, loaded with the library
@@ -106,11 +108,20 @@ def lib():
     L.mxp_gemm_static_capacity.restype = sz
     L.mxp_gemm_workspace_size.argtypes = [i64, i64, i64, i32, i32]
     L.mxp_gemm_workspace_size.restype = sz
+    L.mxp_rmsnorm_quantize.argtypes = [vp, vp, i32, i64, i64, i64, i64, vp, i32, C.c_float, vp, i64, i32, vp, vp, vp, vp]
+    L.mxp_cache_bytes.argtypes = [i64, i64, i64, i64, i32]
+    L.mxp_cache_bytes.restype = sz
+    L.mxp_cache_write.argtypes = [vp, vp, i32, i64, i64, i64, vp, vp, i64, i64, i64, i64, i32, vp]
+    L.mxp_cache_read.argtypes = [vp, i64, i64, i64, i64, i32, vp, i64, vp, vp, i32, i64, i64, vp]
+    L.mxp_attention_workspace_bytes.argtypes = [i64] * 8
+    L.mxp_attention_workspace_bytes.restype = sz
+    L.mxp_attention.argtypes = ([vp, i32, i64, i64, i64, vp, vp, vp, i64, i64, i64, i64, C.c_float, i32, i64, vp, i64, i64, i64, i64, i32] +
+                                [vp, i32, i64, vp, vp, sz, vp])
     L.mxp_status_string.argtypes = [i32]
     L.mxp_status_string.restype = C.c_char_p
     L.mxp_version.restype = i32
     for n in ("mxp_quantize", "mxp_quantize_t", "mxp_dequantize", "mxp_prepack", "mxp_quantize_image", "mxp_prepack_e2m1", "mxp_prepack_e4m3", "mxp_gemm", "mxp_gemm_prepacked",
-              "mxp_gemm_bf16a", "mxp_gemm_decode", "mxp_gemm_decode_bf16a"):
+              "mxp_gemm_bf16a", "mxp_gemm_decode", "mxp_gemm_decode_bf16a", "mxp_rmsnorm_quantize", "mxp_cache_write", "mxp_cache_read", "mxp_attention"):
         getattr(L, n).restype = i32
     _fast = _load_native(L)
     _lib = L
@@ -579,4 +590,157 @@ def gemm_bf16a(a: torch.Tensor, fmt_a, b_image, N: int, out_dtype: torch.dtype =
     ldd = out.stride(0) if M > 1 else max(N, 1)
     _check(lib().mxp_gemm_bf16a(M, N, K, _p(a), _dt(a), lda, fmt_a, _p(b_image), b_kind, _p(out), _dt(out), ldd,
                                 _p(workspace), workspace.numel(), _stream()), "mxp_gemm_bf16a")
+    return out
+
+
+def _here(*tensors):
+    """Tensors (None: left out) of a call lie on the current device, whose current stream the call is enqueued on."""
+    for t in tensors:
+        if t is not None and (not t.is_cuda or t.device.index != torch.cuda.current_device()):
+            raise MxpError("tensors must live on the current GPU")
+
+
+def _like(t: torch.Tensor, shape, dtype, what: str):
+    if tuple(t.shape) != tuple(shape) or t.dtype != dtype:
+        raise MxpError("%s: expected %s of %s, got %s of %s" % (what, dtype, tuple(shape), t.dtype, tuple(t.shape)))
+
+
+def _ld(t: torch.Tensor, what: str) -> int:
+    """Row stride in elements of [rows, ...] whose rows have no gaps inside."""
+    inner = 1
+    for n, st in zip(reversed(t.shape[1:]), reversed(t.stride()[1:])):
+        if n != 1 and st != inner:
+            raise MxpError("%s: rows must be without gaps" % what)
+        inner *= n
+    return t.stride(0) if t.shape[0] > 1 else max(inner, 1)
+
+
+def rmsnorm_quantize(x: torch.Tensor, weight: torch.Tensor, fmt: int = MXFP8, residual: torch.Tensor | None = None, eps: float = 1e-6,
+                     h: torch.Tensor | None = None):
+    """h = x + residual; the root-mean-square norm of h, times weight, quantized -> ((elems, scales, bm_idx), h).
+
+    Without a residual h is x itself, and nothing is written unless h is given; h may be x or residual (in place)."""
+    _here(x, weight, residual, h)
+    _dev2d(x)
+    rows, K = x.shape
+    if weight.shape != (K,) or weight.stride(0) != 1:
+        raise MxpError("weight must be dense, of length %d" % K)
+    for t in (residual, h):
+        if t is not None:
+            _like(_dev2d(t), x.shape, x.dtype, "residual and h")
+    if h is None and residual is not None:
+        h = torch.empty((rows, K), dtype=x.dtype, device=x.device)
+    elems = torch.empty((rows, K * _CODE_BITS.get(fmt, 4) // 8), dtype=torch.uint8, device=x.device)
+    scales = torch.empty((rows, K // 32), dtype=torch.uint8, device=x.device)
+    idx = torch.empty((rows, K // 32), dtype=torch.uint8, device=x.device)
+    _check(lib().mxp_rmsnorm_quantize(_p(x), _p(residual), _dt(x), rows, K, _ld(x, "x"), 0 if residual is None else _ld(residual, "residual"),
+                                      _p(weight), _dt(weight), eps, _p(h), 0 if h is None else _ld(h, "h"), fmt, _p(elems), _p(scales), _p(idx),
+                                      _stream()), "mxp_rmsnorm_quantize")
+    return (elems, scales, idx), x if h is None else h
+
+
+class KVCache(NamedTuple):
+    """The paged cache: data uint8 [n_pages, kv_heads, 2, bytes of a record] and what its bytes are."""
+    data: torch.Tensor
+    page_tokens: int
+    kv_heads: int
+    head_dim: int
+    fmt: int
+
+
+def cache_bytes(n_pages: int, page_tokens: int, kv_heads: int, head_dim: int, fmt: int = MXFP4P) -> int:
+    return int(lib().mxp_cache_bytes(n_pages, page_tokens, kv_heads, head_dim, fmt))
+
+
+def cache_empty(n_pages: int, page_tokens: int, kv_heads: int, head_dim: int, fmt: int = MXFP4P, device=None) -> KVCache:
+    """A cache with nothing in it (its memory is not initialised: only written slots are ever used)."""
+    n = cache_bytes(n_pages, page_tokens, kv_heads, head_dim, fmt)
+    if n == 0:
+        raise MxpError("no cache of %d pages of %d tokens, %d heads of %d, format %d" % (n_pages, page_tokens, kv_heads, head_dim, fmt))
+    data = torch.empty((n_pages, kv_heads, 2, n // (n_pages * kv_heads * 2)), dtype=torch.uint8, device="cuda" if device is None else device)
+    return KVCache(data, page_tokens, kv_heads, head_dim, fmt)
+
+
+def _cache_pages(cache: KVCache) -> int:
+    d = cache.data
+    n = d.shape[0] if d.dim() == 4 else 0
+    if d.dtype != torch.uint8 or not d.is_contiguous() or d.numel() == 0 or d.numel() != cache_bytes(n, *cache[1:]) or d.shape[1] != cache.kv_heads:
+        raise MxpError("the cache's data does not fit its page size, heads and format")
+    return n
+
+
+def _slots(slots: torch.Tensor) -> int:
+    if slots.dtype != torch.int64 or slots.dim() != 1 or not slots.is_contiguous():
+        raise MxpError("slots must be a contiguous 1-D int64 tensor")
+    return slots.numel()
+
+
+def cache_write(cache: KVCache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor):
+    """k, v [tokens, kv_heads, head_dim] fp32/bf16 quantized into the slots (int64, page * page_tokens + place; distinct, but for
+    those outside the cache, -1 say, whose tokens are not kept) of their tokens."""
+    _here(cache.data, k, v, slots)
+    n_pages, n = _cache_pages(cache), _slots(slots)
+    _like(k, (n, cache.kv_heads, cache.head_dim), v.dtype, "k and v")
+    _like(v, k.shape, k.dtype, "k and v")
+    _check(lib().mxp_cache_write(_p(k), _p(v), _dt(k), n, _ld(k, "k"), _ld(v, "v"), _p(slots), _p(cache.data), n_pages, *cache[1:], _stream()),
+           "mxp_cache_write")
+
+
+def cache_read(cache: KVCache, slots: torch.Tensor, dtype: torch.dtype = torch.bfloat16, out=None):
+    """(k, v) [tokens, kv_heads, head_dim] of the given slots, de-converted; zeros for slots outside the cache."""
+    _here(cache.data, slots, *(out or ()))
+    n_pages, n = _cache_pages(cache), _slots(slots)
+    shape = (n, cache.kv_heads, cache.head_dim)
+    k, v = out if out is not None else (torch.empty(shape, dtype=dtype, device=slots.device) for _ in range(2))
+    _like(k, shape, v.dtype, "out")
+    _like(v, shape, k.dtype, "out")
+    _check(lib().mxp_cache_read(_p(cache.data), n_pages, *cache[1:], _p(slots), n, _p(k), _p(v), _dt(k), _ld(k, "k"), _ld(v, "v"), _stream()),
+           "mxp_cache_read")
+    return k, v
+
+
+def attention_workspace_bytes(n_seq: int, rows: int, max_q: int, max_kv: int, heads: int, kv_heads: int, head_dim: int, window: int = 0) -> int:
+    return int(lib().mxp_attention_workspace_bytes(n_seq, rows, max_q, max_kv, heads, kv_heads, head_dim, window))
+
+
+def attention(q: torch.Tensor, cache: KVCache, table: torch.Tensor, kv_len: torch.Tensor, q_start: torch.Tensor | None = None,
+              scale: float | None = None, causal: bool = True, window: int = 0, max_q: int | None = None, max_kv: int | None = None,
+              out_dtype: torch.dtype = torch.bfloat16, out: torch.Tensor | None = None, lse: torch.Tensor | None = None,
+              workspace: torch.Tensor | None = None):
+    """Softmax attention of q [rows, heads, head_dim] bf16 over the cache -> [rows, heads, head_dim].
+
+    table int32 [n_seq, pages]: each sequence's pages; kv_len int32 [n_seq]: its tokens in the cache; q_start int32 [n_seq + 1]: its rows
+    of q (None: one each).  scale: head_dim ** -0.5 if left out.  max_q, max_kv: upper bounds on a sequence's queries and tokens, for
+    the choice of launch (left out: rows, and what the table has room for).  lse fp32 [rows, heads]: takes log-sum-exp of the scores.
+    Rows that belong to no sequence are not written in out and lse."""
+    _here(q, cache.data, table, kv_len, q_start, out, lse, workspace)
+    n_pages = _cache_pages(cache)
+    if q.dim() != 3 or q.shape[2] != cache.head_dim:
+        raise MxpError("q must be [rows, heads, %d]" % cache.head_dim)
+    rows, heads, D = q.shape
+    n_seq = kv_len.numel()
+    if table.dim() != 2 or table.dtype != torch.int32 or table.shape[0] != n_seq or not table.is_contiguous():
+        raise MxpError("table must be a contiguous int32 tensor [n_seq, pages]")
+    for t, n in ((kv_len, n_seq), (q_start, n_seq + 1)):
+        if t is not None and (t.dtype != torch.int32 or t.dim() != 1 or t.numel() != n or not t.is_contiguous()):
+            raise MxpError("kv_len and q_start must be contiguous 1-D int32 tensors of n_seq and n_seq + 1 numbers")
+    if out is None:
+        out = torch.empty((rows, heads, D), dtype=out_dtype, device=q.device)
+    _like(out, q.shape, out.dtype, "out")
+    if lse is not None:
+        _like(lse, (rows, heads), torch.float32, "lse")
+        if not lse.is_contiguous():
+            raise MxpError("lse must be contiguous")
+    if max_q is None:
+        max_q = 1 if q_start is None else rows
+    if max_kv is None:
+        max_kv = min(table.shape[1] * cache.page_tokens, 2 ** 30)
+    if workspace is None:
+        nbytes = attention_workspace_bytes(n_seq, rows, max_q, max_kv, heads, cache.kv_heads, D, window)
+        workspace = torch.empty(nbytes, dtype=torch.uint8, device=q.device) if nbytes else None
+    elif workspace.dtype != torch.uint8 or not workspace.is_contiguous():
+        raise MxpError("workspace must be a contiguous uint8 tensor")
+    _check(lib().mxp_attention(_p(q), _dt(q), _ld(q, "q"), rows, heads, _p(q_start), _p(kv_len), _p(table), table.shape[1], n_seq, max_q, max_kv,
+                               D ** -0.5 if scale is None else scale, int(causal), window, _p(cache.data), n_pages, *cache[1:], _p(out), _dt(out),
+                               _ld(out, "out"), _p(lse), _p(workspace), 0 if workspace is None else workspace.numel(), _stream()), "mxp_attention")
     return out

@@ -1,0 +1,611 @@
+"""The operators around the products of a serving step: norm into block formats, the quantized paged cache, attention over it.
+
+Conversions are compared bit for bit with the CPU oracle, attention with softmax attention in 64 bits on the de-converted cache.
+"""
+import numpy as np
+import pytest
+import torch
+
+import oracle
+from oracle import wide
+from paper_2510_14557_amd import mxp, synth
+
+gpu = pytest.mark.gpu
+FMTS = {"MXFP4": mxp.MXFP4, "MXFP4P": mxp.MXFP4P, "MXFP4PP": mxp.MXFP4PP, "MXFP6": mxp.MXFP6, "MXFP6P": mxp.MXFP6P, "MXFP8": mxp.MXFP8,
+        "MXFP8P": mxp.MXFP8P}
+PLAIN = (mxp.MXFP4, mxp.MXFP6, mxp.MXFP8)
+FOUR = ["MXFP4", "MXFP4P", "MXFP4PP"]
+U = {torch.bfloat16: 2.0 ** -8, torch.float32: 2.0 ** -24}          # half a step, relative
+
+
+def quantize(x, fmt):
+    """Oracle bytes of fp32 rows or bf16 bits."""
+    return oracle.quantize(x, fmt) if fmt <= mxp.MXFP4PP else wide.quantize(x, fmt)
+
+
+def dequantize(q, fmt):
+    return np.asarray(oracle.dequantize(q, fmt) if fmt <= mxp.MXFP4PP else wide.dequantize(q, fmt), dtype=np.float64)
+
+
+def host(t):
+    return t.float().cpu().numpy()
+
+
+def same_bytes(got, want, fmt):
+    e, s, i = (t.cpu().numpy() for t in got)
+    assert (s == want[1]).all() and (e == want[0]).all()
+    if fmt not in PLAIN:
+        assert (i == want[2]).all()
+
+
+# ---- norm -----------------------------------------------------------------------------------------------------------
+SPECIAL = [0.0, -0.0, 1e-39, 2.0 ** -125, -(2.0 ** -124), 7.5, 7.9, -7.0, 5.0, 3.0e38, 0.25, 0.75, 2.5, -3.5, 448.0, 460.0]
+
+
+def special_weight(K, bf16, seed=5):
+    rng = np.random.default_rng(seed)
+    w = (rng.standard_normal(K) * np.exp2(rng.integers(-3, 4, K))).astype(np.float32)
+    for b in range(0, K - 31, 32):
+        kind = b // 32 % 7
+        if kind == 0:
+            w[b:b + 32] = 0.0
+            w[b + 3] = SPECIAL[b // 32 % len(SPECIAL)]
+        elif kind == 1:
+            w[b:b + 32] = rng.choice(SPECIAL[5:], 32)
+        elif kind == 2:
+            w[b + 7] = [np.inf, np.nan, -np.inf][b // 32 % 3]
+        elif kind == 3:
+            w[b:b + 32] *= np.float32(2.0 ** -122)
+        elif kind == 4:
+            w[b + 9] *= 2.0 ** 9
+    return synth.bf16_bits_to_f32(synth.f32_to_bf16_bits(w)) if bf16 else w
+
+
+@gpu
+@pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("K", [32, 512, 4096, 16384, 32768])
+@pytest.mark.parametrize("dt", [torch.bfloat16, torch.float32])
+def test_norm_of_signs_is_the_weight_bit_for_bit(fmt, K, dt):
+    """Rows of +-2^a have the root mean square 2^a exactly (K a power of two, sums below 2^24): y = +-weight, special values included."""
+    f = FMTS[fmt]
+    rng = np.random.default_rng(K)
+    sign = rng.choice([-1.0, 1.0], (3, K)).astype(np.float32)
+    x = torch.from_numpy(sign * np.array([[1.0], [4.0], [0.125]], np.float32)).to("cuda", dt)
+    w = special_weight(K, dt == torch.bfloat16)
+    q, h = mxp.rmsnorm_quantize(x, torch.from_numpy(w).to("cuda", dt), f, eps=0.0)
+    assert h is x
+    with np.errstate(invalid="ignore"):
+        same_bytes(q, quantize(sign * w, f), f)
+
+
+@gpu
+@pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("rows,K", [(1, 4096), (5, 32), (37, 1056), (3, 16384), (2, 16416), (2, 33056)])
+@pytest.mark.parametrize("dt", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("residual", [False, True])
+def test_norm_against_64_bits(fmt, rows, K, dt, residual):
+    """Quantized values lie between those of y (1 - d) and y (1 + d): a lane sums at most 33056 / 1024 / 8 < 5 groups of 8 squares in a
+    row and ten partial sums follow, so the sum is within 64 * 2^-24, y within half of that and four roundings: d = 2^-18."""
+    f = FMTS[fmt]
+    x = torch.from_numpy(synth.activations(rows, K, 1, 3, dtype="f32")).to("cuda", dt)
+    r = torch.from_numpy(synth.activations(rows, K, 1, 4, dtype="f32")).to("cuda", dt) if residual else None
+    w = (1 + 0.1 * torch.randn(K, generator=torch.Generator().manual_seed(K))).to("cuda", dt)
+    q, h = mxp.rmsnorm_quantize(x, w, f, residual=r, eps=1e-5)
+    want_h = (x.float() + r.float()).to(dt) if residual else x
+    assert torch.equal(h, want_h)
+    a = h.double().cpu().numpy()
+    y = a / np.sqrt((a * a).mean(-1, keepdims=True) + 1e-5) * w.double().cpu().numpy()
+    ends = [dequantize(quantize((y * (1 + d)).astype(np.float32), f), f) for d in (-2.0 ** -18, 2.0 ** -18)]
+    got = dequantize(tuple(t.cpu().numpy() for t in q), f)
+    assert (got >= np.minimum(*ends)).all() and (got <= np.maximum(*ends)).all()
+
+
+@gpu
+def test_norm_in_place_strided_and_rows_of_nothing():
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    for K in (2048, 20000):                                       # in registers, in two passes
+        wide_x = torch.randn((9, K + 64), generator=gen, device="cuda").bfloat16()
+        wide_r = torch.randn((9, K + 32), generator=gen, device="cuda").bfloat16()
+        w = torch.randn(K, generator=gen, device="cuda").bfloat16()
+        x, r = wide_x[:, 32:32 + K], wide_r[:, :K]
+        want_q, want_h = mxp.rmsnorm_quantize(x.contiguous(), w, mxp.MXFP8P, residual=r.contiguous())
+        keep = wide_x.clone(), wide_r.clone()
+        for out in (r, x):                                        # h over the residual, then over x (from the values before)
+            wide_x.copy_(keep[0]); wide_r.copy_(keep[1])
+            q, h = mxp.rmsnorm_quantize(x, w, mxp.MXFP8P, residual=r, h=out)
+            assert h is out and torch.equal(out, want_h) and all(torch.equal(a, b) for a, b in zip(q, want_q))
+        assert torch.equal(wide_x[:, :32], keep[0][:, :32]) and torch.equal(wide_x[:, 32 + K:], keep[0][:, 32 + K:])
+        assert torch.equal(wide_r[:, K:], keep[1][:, K:])
+        copy = torch.empty_like(want_h)                           # h without a residual: a copy of x
+        mxp.rmsnorm_quantize(keep[0][:, 32:32 + K], w, mxp.MXFP8P, h=copy)
+        assert torch.equal(copy, keep[0][:, 32:32 + K])
+    z = torch.zeros((4, 64), device="cuda")
+    z[1, 3], z[2, 40] = float("nan"), float("inf")
+    (e, s, i), _ = mxp.rmsnorm_quantize(z, torch.ones(64, device="cuda"), mxp.MXFP4P, eps=1e-6)
+    assert s.tolist() == [[0, 0], [255, 255], [0, 255], [0, 0]]   # NaN spoils the row; Inf: others 0 / Inf, itself NaN
+    (e, s, i), _ = mxp.rmsnorm_quantize(z[3:], torch.ones(64, device="cuda"), mxp.MXFP4P, eps=0.0)
+    assert s.tolist() == [[255, 255]]                             # 0 / 0
+    for shape in ((0, 64), (3, 0)):
+        (e, s, i), _ = mxp.rmsnorm_quantize(torch.empty(shape, device="cuda"), torch.empty(shape[1], device="cuda"), mxp.MXFP8)
+        assert e.shape[0] == shape[0] and e.numel() == 0
+
+
+# ---- the cache ------------------------------------------------------------------------------------------------------
+def records(e, s, i, n_pages, T, H, D, fmt):
+    """Oracle bytes of rows [page][token][head] as the cache's records [page][head][bytes]."""
+    parts = []
+    for a, width in ((e, D // 2), (s, D // 32), (i, D // 32))[:2 if fmt == mxp.MXFP4 else 3]:
+        parts.append(a.reshape(n_pages, T, H, width).transpose(0, 2, 1, 3).reshape(n_pages, H, T * width))
+    return np.concatenate(parts, -1)
+
+
+@gpu
+@pytest.mark.parametrize("fmt", FOUR)
+@pytest.mark.parametrize("dt", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("T,H,D,n", [(16, 1, 64, 1), (16, 8, 128, 77), (64, 3, 128, 200), (256, 5, 64, 311), (32, 2, 256, 50), (128, 7, 256, 3)])
+def test_cache_write_and_read_bit_for_bit(fmt, dt, T, H, D, n):
+    f = FMTS[fmt]
+    rng = np.random.default_rng(n)
+    n_pages = n // T + 3
+    slots = rng.permutation(n_pages * T)[:n].astype(np.int64)
+    qkv = synth.activations(n, 3 * H * D, 2, n % 7, dtype="f32").reshape(n, 3 * H, D)
+    qkv[:, :, :32] *= np.exp2(rng.integers(-130, 100, (n, 3 * H, 1))).astype(np.float32)
+    qkv[0, :, 32:64] = 0
+    qkv[-1, 1::2, 40], qkv[-1, ::2, 33] = np.inf, np.nan
+    x = torch.from_numpy(qkv).to("cuda", dt)
+    k, v = x[:, H:2 * H], x[:, 2 * H:]                            # slices of a joint projection
+    bits = synth.f32_to_bf16_bits(qkv) if dt == torch.bfloat16 else qkv
+    skipped = slots.copy()
+    skipped[::5] = [-1, n_pages * T, -(2 ** 40), 2 ** 40][n % 4]
+    cache = mxp.cache_empty(n_pages, T, H, D, f)
+    cache.data.fill_(0xA5)
+    mxp.cache_write(cache, k, v, torch.from_numpy(skipped).cuda())
+    kept = skipped == slots
+    want = np.full(tuple(cache.data.shape), 0xA5, np.uint8)
+    values = []
+    for part, rows in ((0, bits[:, H:2 * H]), (1, bits[:, 2 * H:])):
+        e, s, i = oracle.quantize(np.ascontiguousarray(rows).reshape(n * H, D), f)
+        values.append(oracle.dequantize((e, s, i), f).reshape(n, H, D))
+        full = []
+        for a in (e, s, i):
+            b = np.full((n_pages * T, H, a.shape[1]), 0xA5, np.uint8)
+            b[slots[kept]] = a.reshape(n, H, -1)[kept]
+            full.append(b)
+        want[:, :, part] = records(*full, n_pages, T, H, D, f)
+    assert (cache.data.cpu().numpy() == want).all()
+    for out_dt in (torch.bfloat16, torch.float32):
+        room = torch.full((n, 2 * H + 1, D), 7.0, dtype=out_dt, device="cuda")
+        got = mxp.cache_read(cache, torch.from_numpy(skipped).cuda(), out=(room[:, :H], room[:, H:2 * H]))
+        for g, val in zip(got, values):
+            np.testing.assert_array_equal(g.double().cpu().numpy(), np.where(kept[:, None, None], val, 0.0))
+        assert (room[:, 2 * H] == 7).all()
+    twice = torch.from_numpy(np.repeat(slots[kept][:1], 5)).cuda()   # a slot may be read more than once
+    np.testing.assert_array_equal(mxp.cache_read(cache, twice, torch.float32)[1].double().cpu().numpy(), np.repeat(values[1][kept][:1], 5, 0))
+
+
+@gpu
+def test_cache_beyond_32_bit_offsets():
+    """Pages above 4 GiB: written, read and attended to as the first ones are."""
+    T, H, D, f = 256, 8, 128, mxp.MXFP4P
+    n_pages = 18500
+    size = mxp.cache_bytes(n_pages, T, H, D, f)
+    assert size > 5 << 30
+    cache = mxp.cache_empty(n_pages, T, H, D, f)
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    k, v = (torch.randn((300, H, D), generator=gen, device="cuda").bfloat16() for _ in range(2))
+    q = torch.randn((1, 16, D), generator=gen, device="cuda").bfloat16()
+    kv_len = torch.tensor([300], dtype=torch.int32, device="cuda")
+    outs = []
+    for pages in ((0, 1), (n_pages - 1, n_pages - 2)):
+        table = torch.tensor([pages], dtype=torch.int32, device="cuda")
+        t = torch.arange(300, device="cuda")
+        slots = table[0, t // T].long() * T + t % T
+        mxp.cache_write(cache, k, v, slots)
+        outs.append(mxp.cache_read(cache, slots, torch.float32) + (mxp.attention(q, cache, table, kv_len, out_dtype=torch.float32),))
+    assert all(torch.equal(a, b) for a, b in zip(*outs))
+
+
+# ---- attention ------------------------------------------------------------------------------------------------------
+class Batch:
+    """Sequences in a cache of quantized random rows; every slot that no sequence has is poisoned with NaN blocks."""
+
+    def __init__(self, fmt, T, H, G, D, kv, nq, seed=0, gaps=False, garbage=True):
+        rng = np.random.default_rng(seed)
+        self.f, self.T, self.H, self.G, self.D, self.kv, self.nq = FMTS[fmt], T, H, G, D, kv, nq
+        per = [-(-n // T) for n in kv]
+        self.n_pages = n_pages = sum(per) + 2
+        names = rng.permutation(n_pages)
+        self.table = np.full((len(kv), max(max(per), 1) + 1), -1, np.int32)
+        at = 0
+        for s, p in enumerate(per):
+            self.table[s, :p] = names[at:at + p]
+            at += p
+        raw = rng.standard_normal((2, n_pages * T * H, D)).astype(np.float32)
+        raw[0] *= np.where(rng.random((1, D)) < 0.05, 6.0, 1.0).astype(np.float32)
+        self.q3 = [oracle.quantize(r, self.f) for r in raw]
+        self.val = [oracle.dequantize(q, self.f).reshape(n_pages * T, H, D) for q in self.q3]
+        self.slots = [self.table[s, np.arange(n) // T].astype(np.int64) * T + np.arange(n) % T for s, n in enumerate(kv)]
+        if garbage:
+            free = np.ones(n_pages * T, bool)
+            for sl in self.slots:
+                free[sl] = False
+            for e, sc, ix in self.q3:
+                sc.reshape(n_pages * T, H, -1)[free] = 255
+        self.start = np.concatenate([[0], np.cumsum(nq)]).astype(np.int32)
+        self.q = torch.from_numpy(rng.standard_normal((int(self.start[-1]), H * G, D)).astype(np.float32)).bfloat16().cuda()
+
+    def poison(self, seq, t, blocks, part):
+        """NaN blocks in a visible token's keys (0) or values (1)."""
+        slot = self.slots[seq][t]
+        self.q3[part][1].reshape(self.n_pages * self.T, self.H, -1)[slot, :, blocks] = 255
+        for b in blocks:
+            self.val[part][slot, :, 32 * b:32 * b + 32] = np.nan
+
+    def cache(self):
+        data = np.stack([records(*q, self.n_pages, self.T, self.H, self.D, self.f) for q in self.q3], 2)
+        return mxp.KVCache(torch.from_numpy(np.ascontiguousarray(data)).cuda(), self.T, self.H, self.D, self.f)
+
+    def call(self, cache=None, **kw):
+        n = len(self.kv)
+        kw.setdefault("lse", torch.full((self.q.shape[0], self.H * self.G), 77.0, device="cuda"))
+        kw.setdefault("max_q", max(self.nq + [1]))
+        kw.setdefault("max_kv", max(self.kv))
+        out = mxp.attention(kw.pop("q", self.q), cache or self.cache(), torch.from_numpy(self.table).cuda(),
+                            torch.tensor(self.kv, dtype=torch.int32, device="cuda"),
+                            q_start=None if self.nq == [1] * n else torch.from_numpy(self.start).cuda(), **kw)
+        return out, kw["lse"]
+
+    def check(self, out, lse, causal=True, window=0, scale=None, hidden=lambda s: None):
+        """Against 64 bits.  An output is off by at most
+            2 e S + p S + a S + u |o|,    S = sum p |v| / sum p,
+        e: a score's error, 2 (D + 8) 2^-24 of the largest visible scale * sum |q k| (the product's sums and the roundings behind it),
+        once in p and once in the sum; p: the rounding of p to one bf16 term (2^-8, bf16 output) or two (2^-16); a: fp32 sums over the
+        tokens and joins, (tokens + 64) 2^-24, exp2 and the division in the 64; u: the output's own rounding."""
+        scale = self.D ** -0.5 if scale is None else scale
+        got, got_lse, qh = out.double().cpu().numpy(), lse.double().cpu().numpy(), self.q.double().cpu().numpy()
+        p_err, u = (2.0 ** -8, U[torch.bfloat16]) if out.dtype == torch.bfloat16 else (2.0 ** -16, U[torch.float32])
+        for s, n in enumerate(self.kv):
+            m, rows = self.nq[s], slice(int(self.start[s]), int(self.start[s + 1]))
+            k, v = (x[self.slots[s]].transpose(1, 0, 2) for x in self.val)         # [H][n][D]
+            q = qh[rows].reshape(m, self.H, self.G, self.D).transpose(1, 0, 2, 3).reshape(self.H, m * self.G, self.D)
+            pos = (n - m + np.arange(m) if causal else np.full(m, n - 1)).repeat(self.G)[None, :, None]
+            t = np.arange(n)
+            seen = np.broadcast_to((t <= pos) & ((t > pos - window) if window else True), (self.H, m * self.G, n)).copy()
+            if hidden(s) is not None:
+                seen[:, :, hidden(s)] = False
+            z = np.where(seen, scale * (q @ k.transpose(0, 2, 1)), -np.inf)
+            size = np.where(seen, abs(scale) * (abs(q) @ abs(k).transpose(0, 2, 1)), 0.0).max(-1, initial=0.0)
+            with np.errstate(invalid="ignore", divide="ignore"):
+                top = z.max(-1, initial=-np.inf)
+                p = np.where(seen, np.exp(z - np.where(np.isneginf(top), 0.0, top)[..., None]), 0.0)
+                total = p.sum(-1)
+                d = np.where(total == 0, 1.0, total)[..., None]
+                if np.isnan(v).any():                                              # an invisible token's values do not count
+                    bad = np.isnan(v)
+                    o = p @ np.where(bad, 0.0, v) / d
+                    o[(seen.astype(float) @ bad.astype(float)) > 0] = np.nan
+                    S = p @ np.where(bad, 0.0, abs(v)) / d
+                else:
+                    o, S = p @ v / d, p @ abs(v) / d
+                want_lse = np.where(total == 0, -np.inf, top + np.log(total))
+            e = 2 * (self.D + 8) * 2.0 ** -24 * size
+            a = (n + 64) * 2.0 ** -24
+            tol = (2 * e[..., None] + p_err + a) * S + u * abs(o)
+            shape = lambda x: x.reshape((self.H, m, self.G) + x.shape[2:]).swapaxes(0, 1).reshape((m, self.H * self.G) + x.shape[2:])
+            o, tol, want_lse, lse_tol = (shape(x) for x in (o, tol, want_lse, e + a + abs(np.where(np.isfinite(want_lse), want_lse, 0)) * 2.0 ** -22))
+            g, gl = got[rows], got_lse[rows]
+            assert (np.isnan(g) == np.isnan(o)).all() and (np.isnan(gl) == np.isnan(want_lse)).all()
+            ok = ~np.isnan(o)
+            assert (abs(g - o)[ok] <= tol[ok]).all(), (s, (abs(g - o) / tol)[ok].max())
+            fine = np.isfinite(want_lse)
+            assert (gl[~fine & ~np.isnan(want_lse)] == -np.inf).all()
+            off = abs(gl[fine] - want_lse[fine]) / lse_tol[fine]
+            assert (off <= 1).all(), (s, off.max())
+
+
+ODD = [1, 15, 16, 17, 31, 33, 63, 64, 65, 100, 129, 255, 257, 600]
+
+
+@gpu
+@pytest.mark.parametrize("out", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("fmt", FOUR)
+@pytest.mark.parametrize("D,T,H,G", [(64, 16, 2, 1), (128, 16, 2, 4), (128, 64, 1, 8), (256, 32, 1, 16), (64, 256, 3, 7), (128, 32, 1, 20), (256, 128, 2, 17)])
+def test_attention_one_query_each(out, fmt, D, T, H, G):
+    b = Batch(fmt, T, H, G, D, ODD, [1] * len(ODD), seed=D + G)
+    b.check(*b.call(out_dtype=out))
+
+
+@gpu
+@pytest.mark.parametrize("out", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("fmt", FOUR)
+@pytest.mark.parametrize("D,T,H,G", [(64, 32, 2, 3), (128, 16, 1, 4), (256, 16, 1, 2), (128, 128, 2, 1)])
+@pytest.mark.parametrize("window", [0, 40])
+def test_attention_ragged_queries(out, fmt, D, T, H, G, window):
+    """A few queries (one workgroup's rows), many, none, and more queries than tokens: the first of them see nothing."""
+    for kv, nq in (([5, 40, 0, 333, 64], [5, 3, 2, 8, 0]), ([300, 130, 7, 64, 1], [300, 41, 20, 64, 1]), ([70], [130])):
+        b = Batch(fmt, T, H, G, D, kv, nq, seed=window + G)
+        b.check(*b.call(out_dtype=out, window=window), window=window)
+
+
+@gpu
+@pytest.mark.parametrize("nq", [[1, 1], [6, 40]])
+def test_attention_not_causal_and_other_scales(nq):
+    b = Batch("MXFP4P", 16, 2, 4, 128, [77, 200], nq, seed=3)
+    b.check(*b.call(causal=False, scale=0.3, out_dtype=torch.float32), causal=False, scale=0.3)
+    b.check(*b.call(scale=-0.2), scale=-0.2)
+    b.check(*b.call(scale=0.0), scale=0.0)
+
+
+@gpu
+@pytest.mark.parametrize("G,n", [(1, 1), (4, 2), (4, 50)])
+def test_attention_splits_long_sequences(G, n):
+    """Long sequences next to short and empty ones: parts without a visible token among them."""
+    kv = [5000, 3, 0, 777, 2049]
+    b = Batch("MXFP4P", 64, 2, G, 128, kv, [n, n, 1, n, n], seed=n)
+    rows = int(b.start[-1])
+    assert mxp.attention_workspace_bytes(5, rows, n, 5000, 2 * G, 2, 128) > 0
+    out, lse = b.call(out_dtype=torch.float32)
+    b.check(out, lse)
+    again = b.call(out_dtype=torch.float32)
+    assert torch.equal(out, again[0]) and torch.equal(lse, again[1])              # no order that changes
+    b.check(*b.call(window=300), window=300)
+
+
+@gpu
+@pytest.mark.parametrize("n", [1, 4, 60])
+def test_attention_bounds_are_hints(n):
+    """Bounds below the true sizes change the launch, not the result; bounds far above them neither."""
+    b = Batch("MXFP4", 16, 1, 4, 64, [700, 90], [n, n], seed=9)
+    for max_q, max_kv in ((1, 1), (n, 100), (1, 700), (5000, 1 << 20), (0, 0)):
+        b.check(*b.call(max_q=max_q, max_kv=max_kv, out_dtype=torch.float32))
+
+
+@gpu
+@pytest.mark.parametrize("n", [1, 3, 70])
+def test_attention_pages_that_are_not_there(n):
+    """Entries outside the cache hide their tokens; the last page's tokens behind kv_len hold NaN blocks throughout."""
+    b = Batch("MXFP4P", 16, 2, 2, 128, [200, 95, 33], [n] * 3, seed=4)
+    gone = {0: [0, 3, 12], 1: [1], 2: [0, 1, 2]}
+    for s, pages in gone.items():
+        b.table[s, pages] = [-1, b.n_pages, 2 ** 31 - 1][s]
+    hide = lambda s: [t for t in range(b.kv[s]) if t // 16 in gone[s]]
+    for out in (torch.bfloat16, torch.float32):
+        o, lse = b.call(out_dtype=out)
+        b.check(o, lse, hidden=hide)
+        if n <= 33:
+            assert (o[2 * n:] == 0).all() and (lse[2 * n:] == -float("inf")).all()
+
+
+@gpu
+@pytest.mark.parametrize("G,n", [(2, 1), (2, 6), (4, 90)])
+@pytest.mark.parametrize("D", [64, 128, 256])
+def test_attention_nan_blocks_count_where_they_are_seen(G, n, D):
+    """NaN blocks of keys and values in the last tokens: the queries before them are not touched."""
+    b = Batch("MXFP4P", 16, 2, G, D, [150, 95], [n, n], seed=6)
+    b.poison(0, 150 - (n + 1) // 2, [1], 1)
+    b.poison(0, 149, [0], 1)
+    b.poison(1, 94, [D // 32 - 1], 0)
+    o, lse = b.call(out_dtype=torch.float32)
+    b.check(o, lse)
+    if n > 1:
+        assert not o[0].isnan().any() and not o[n].isnan().any()
+
+
+@gpu
+def test_attention_strides_rows_of_no_sequence_and_device_side_lengths():
+    """q a slice of a joint projection, out with gaps; rows before the first and behind the last sequence stay as they are."""
+    b = Batch("MXFP4P", 32, 2, 3, 64, [50, 120], [4, 30], seed=8)
+    joint = torch.full((40, 10, 64), float("nan"), device="cuda").bfloat16()
+    joint[3:37, 2:8] = b.q
+    for dt in (torch.bfloat16, torch.float32):
+        room = torch.full((40, 8, 64), 5.0, dtype=dt, device="cuda")
+        lse = torch.full((40, 6), 5.0, device="cuda")
+        start = torch.from_numpy(b.start + 3).cuda()
+        mxp.attention(joint[:, 2:8], b.cache(), torch.from_numpy(b.table).cuda(), torch.tensor(b.kv, dtype=torch.int32, device="cuda"),
+                      q_start=start, max_q=30, max_kv=120, out=room[:, 1:7], lse=lse)
+        b.check(room[3:37, 1:7], lse[3:37])
+        assert (room[:3] == 5).all() and (room[37:] == 5).all() and (room[:, 0] == 5).all() and (room[:, 7] == 5).all()
+        assert (lse[:3] == 5).all() and (lse[37:] == 5).all()
+    none = mxp.attention(b.q[:0], b.cache(), torch.from_numpy(b.table).cuda()[:0], torch.empty(0, dtype=torch.int32, device="cuda"))
+    assert none.shape == (0, 6, 64)
+
+
+@gpu
+def test_attention_large_scores_and_flushed_blocks():
+    """Scores in the hundreds, one key far ahead of all others, blocks of zeros: the running maximum carries them."""
+    b = Batch("MXFP4P", 16, 1, 4, 128, [400, 400], [1, 60], seed=11, garbage=False)
+    b.q *= 30
+    for part in (0, 1):
+        sc = b.q3[part][1]
+        sc[::7] = 0
+        b.q3[part][0].reshape(len(sc), -1, 16)[::7] = 0
+        b.q3[part][2][::7] = 0
+        b.val[part] = oracle.dequantize(b.q3[part], b.f).reshape(b.val[part].shape)
+    for out in (torch.bfloat16, torch.float32):
+        b.check(*b.call(out_dtype=out))
+
+
+# ---- together -------------------------------------------------------------------------------------------------------
+def test_refusals_before_anything_is_launched():
+    """Status codes of the entry points for what they do not take, on the CPU: nothing is enqueued."""
+    import ctypes as C
+    L = mxp.lib()
+    buf = (C.c_uint8 * 4096)()
+    addr = (C.addressof(buf) + 15) & ~15
+    p, odd, N = C.c_void_p(addr), C.c_void_p(addr + 2), None
+    B, F = mxp.BF16, mxp.F32
+    norm = lambda x=p, r=p, dt=B, rows=4, K=64, lx=64, lr=64, w=p, wd=B, eps=1e-6, h=p, lh=64, f=mxp.MXFP8, e=p, s=p, i=p: \
+        L.mxp_rmsnorm_quantize(x, r, dt, rows, K, lx, lr, w, wd, eps, h, lh, f, e, s, i, None)
+    assert norm(f=7) == -5 and norm(f=-1) == -5 and norm(dt=2) == -4 and norm(wd=2) == -4
+    assert norm(K=48) == -2 and norm(rows=-1) == -2 and norm(eps=-1.0) == -2 and norm(eps=float("nan")) == -2 and norm(eps=float("inf")) == -2
+    assert norm(lx=32) == -2 and norm(lr=32) == -2 and norm(lh=32) == -2
+    assert norm(x=N) == -1 and norm(w=N) == -1 and norm(e=N) == -1 and norm(s=N) == -1 and norm(f=mxp.MXFP8P, i=N) == -1
+    assert norm(x=odd) == -3 and norm(r=odd) == -3 and norm(h=odd) == -3 and norm(w=odd) == -3 and norm(lx=68) == -3 and norm(e=odd) == -3
+    assert norm(K=(1 << 21) + 32, lx=1 << 22, lr=1 << 22, lh=1 << 22) == -8 and norm(rows=0, x=N) == 0 and norm(K=0, x=N) == 0
+
+    size = lambda n=4, T=16, H=2, D=128, f=1: L.mxp_cache_bytes(n, T, H, D, f)
+    assert size() == 4 * 2 * 2 * 16 * 72 and size(f=0) == 4 * 2 * 2 * 16 * 68
+    assert [size(n=0), size(T=8), size(T=48), size(T=512), size(H=0), size(D=96), size(D=0), size(f=5), size(f=9)] == [0] * 9
+    for call in (lambda k=p, v=p, dt=B, n=3, lk=256, lv=256, sl=p, c=p, pages=4, T=16, H=2, D=128, f=1: L.mxp_cache_write(k, v, dt, n, lk, lv, sl, c, pages, T, H, D, f, None),
+                 lambda k=p, v=p, dt=B, n=3, lk=256, lv=256, sl=p, c=p, pages=4, T=16, H=2, D=128, f=1: L.mxp_cache_read(c, pages, T, H, D, f, sl, n, k, v, dt, lk, lv, None)):
+        assert call(f=3) == -8 and call(f=8) == -5 and call(T=17) == -8 and call(D=32) == -8 and call(pages=0) == -2 and call(H=0) == -2
+        assert call(dt=3) == -4 and call(n=-1) == -2 and call(lk=255) == -2 and call(lv=128) == -2 and call(lk=260) == -3
+        assert call(k=N) == -1 and call(v=N) == -1 and call(sl=N) == -1 and call(c=N) == -1 and call(n=0, k=N) == 0
+        assert call(k=odd) == -3 and call(c=odd) == -3 and call(sl=odd) == -3
+
+    def attn(Q=p, qd=B, lq=1024, rows=3, heads=8, qs=p, kl=p, tb=p, lt=4, n=2, mq=3, mk=64, scale=0.1, causal=1, win=0, c=p, pages=4, T=16, H=2, D=128, f=1,
+             O=p, od=B, lo=1024, lse=p, ws=N, wb=0):
+        return L.mxp_attention(Q, qd, lq, rows, heads, qs, kl, tb, lt, n, mq, mk, scale, causal, win, c, pages, T, H, D, f, O, od, lo, lse, ws, wb, None)
+    assert attn(f=6) == -8 and attn(f=11) == -5 and attn(D=96) == -8 and attn(T=8) == -8 and attn(pages=0) == -2
+    assert attn(qd=5) == -4 and attn(od=5) == -4 and attn(qd=F) == -8
+    assert attn(heads=7) == -2 and attn(heads=0) == -2 and attn(rows=-1) == -2 and attn(mq=-1) == -2 and attn(mk=-1) == -2 and attn(win=-1) == -2
+    assert attn(causal=0, win=5) == -2 and attn(scale=float("inf")) == -2 and attn(scale=float("nan")) == -2 and attn(lt=-1) == -2
+    assert attn(qs=N) == -2                                       # one row per sequence, and three rows for two
+    assert attn(lq=1000) == -2 and attn(lo=512) == -2 and attn(lq=1028) == -3 and attn(lo=1028) == -3
+    assert [attn(Q=N), attn(kl=N), attn(tb=N), attn(c=N), attn(O=N)] == [-1] * 5
+    assert [attn(Q=odd), attn(O=odd), attn(c=odd), attn(qs=odd), attn(kl=odd), attn(tb=odd), attn(lse=odd)] == [-3] * 7
+    assert attn(rows=1 << 28) == -8 and attn(rows=0, Q=N) == 0 and attn(n=0, Q=N) == 0
+    need = mxp.attention_workspace_bytes(2, 3, 3, 100000, 8, 2, 128)
+    assert need > 0 and attn(mk=100000) == -6 and attn(mk=100000, ws=p, wb=need - 1) == -6
+    assert mxp.attention_workspace_bytes(0, 3, 3, 100000, 8, 2, 128) == 0 == mxp.attention_workspace_bytes(2, 3, 3, 100000, 7, 2, 128)
+
+
+def test_binding_refuses_what_does_not_fit():
+    """Tensors elsewhere than on the current GPU, and with no GPU at all: an exception, never another route."""
+    x = torch.zeros((4, 64))
+    c = mxp.KVCache(torch.zeros((4, 2, 2, 16 * 36), dtype=torch.uint8), 16, 2, 64, mxp.MXFP4P)
+    i32 = lambda *s: torch.zeros(s, dtype=torch.int32)
+    for call in (lambda: mxp.rmsnorm_quantize(x, x[0]), lambda: mxp.cache_write(c, x.view(2, 2, 64), x.view(2, 2, 64), torch.zeros(2, dtype=torch.int64)),
+                 lambda: mxp.cache_read(c, torch.zeros(2, dtype=torch.int64)),
+                 lambda: mxp.attention(torch.zeros((1, 2, 64)).bfloat16(), c, i32(1, 1), i32(1))):
+        with pytest.raises(mxp.MxpError, match="current GPU"):
+            call()
+    with pytest.raises(mxp.MxpError, match="no cache"):
+        mxp.cache_empty(4, 24, 2, 64)
+
+
+@gpu
+def test_binding_refuses_shapes_and_types():
+    z = lambda *s, dt=torch.bfloat16: torch.zeros(s, dtype=dt, device="cuda")
+    c = mxp.cache_empty(4, 16, 2, 64)
+    i32 = lambda *s: z(*s, dt=torch.int32)
+    sl = z(3, dt=torch.int64)
+    k = z(3, 2, 64)
+    bad = [lambda: mxp.rmsnorm_quantize(z(4, 64), z(32)), lambda: mxp.rmsnorm_quantize(z(4, 64), z(64), residual=z(4, 64, dt=torch.float32)),
+           lambda: mxp.rmsnorm_quantize(z(4, 64), z(64), residual=z(3, 64)), lambda: mxp.rmsnorm_quantize(z(4, 48), z(48)),
+           lambda: mxp.rmsnorm_quantize(z(64, 4).t(), z(64)), lambda: mxp.rmsnorm_quantize(z(4, 64), z(64), eps=-1.0),
+           lambda: mxp.cache_write(c, k, k, sl.int()), lambda: mxp.cache_write(c, k, k.float(), sl), lambda: mxp.cache_write(c, k, k[:2], sl),
+           lambda: mxp.cache_write(c, z(3, 64, 2).transpose(1, 2), k, sl), lambda: mxp.cache_write(c._replace(page_tokens=32), k, k, sl),
+           lambda: mxp.cache_write(c._replace(data=c.data.flatten()), k, k, sl), lambda: mxp.cache_write(c._replace(fmt=mxp.MXFP4), k, k, sl),
+           lambda: mxp.cache_read(c, sl[::2]), lambda: mxp.cache_read(c, sl, out=(k, k.float())),
+           lambda: mxp.attention(z(1, 4, 128), c, i32(1, 1), i32(1)), lambda: mxp.attention(z(1, 4, 64), c, i32(2, 1), i32(1)),
+           lambda: mxp.attention(z(1, 4, 64), c, z(1, 1, dt=torch.int64), i32(1)), lambda: mxp.attention(z(1, 4, 64), c, i32(1, 1), i32(1), q_start=i32(1)),
+           lambda: mxp.attention(z(2, 4, 64), c, i32(1, 1), i32(1)), lambda: mxp.attention(z(1, 3, 64), c, i32(1, 1), i32(1)),
+           lambda: mxp.attention(z(1, 4, 64, dt=torch.float32), c, i32(1, 1), i32(1)), lambda: mxp.attention(z(1, 4, 64), c, i32(1, 1), i32(1), lse=z(1, 4)),
+           lambda: mxp.attention(z(1, 4, 64), c, i32(1, 1), i32(1), causal=False, window=3),
+           lambda: mxp.attention(z(1, 4, 64), c, i32(1, 4000), i32(1), workspace=z(16, dt=torch.uint8))]
+    for n, call in enumerate(bad):
+        with pytest.raises((mxp.MxpError, TypeError)):
+            call()
+            pytest.fail("call %d was taken" % n)
+
+
+class Layer:
+    """The attention half of a layer as a serving program runs it: norm, joint projection, cache, attention, next residual."""
+
+    def __init__(self, n_seq=3, H=2, G=2, D=64, T=16, pages=6):
+        gen = torch.Generator(device="cuda").manual_seed(0)
+        self.H, self.G, self.D, self.T, self.n = H, G, D, T, n_seq
+        K = 256
+        self.w = (1 + 0.1 * torch.randn(K, generator=gen, device="cuda")).bfloat16()
+        self.qw = mxp.quantize((torch.randn(((G + 2) * H * D, K), generator=gen, device="cuda") * 0.06).bfloat16(), mxp.MXFP4P)
+        self.cache = mxp.cache_empty(n_seq * pages, T, H, D)
+        self.table = torch.randperm(n_seq * pages, generator=gen, device="cuda").to(torch.int32).view(n_seq, pages)
+        self.kv_len = torch.zeros(n_seq, dtype=torch.int32, device="cuda")
+        self.x, self.r = (torch.randn((n_seq, K), generator=gen, device="cuda").bfloat16() for _ in range(2))
+        need = mxp.attention_workspace_bytes(n_seq, n_seq, 1, pages * T, G * H, H, D)
+        self.ws = torch.empty(max(need, 16), dtype=torch.uint8, device="cuda")
+
+    def step(self):
+        q8, self.h = mxp.rmsnorm_quantize(self.x, self.w, mxp.MXFP8, residual=self.r)
+        self.act = q8
+        self.qkv = mxp.gemm(q8, mxp.MXFP8, self.qw, mxp.MXFP4P, torch.bfloat16).view(self.n, -1, self.D)
+        t = self.kv_len.long()
+        slots = self.table.gather(1, (t // self.T)[:, None])[:, 0].long() * self.T + t % self.T
+        HG = self.H * self.G
+        mxp.cache_write(self.cache, self.qkv[:, HG:HG + self.H], self.qkv[:, HG + self.H:], slots)
+        self.kv_len += 1
+        self.o = mxp.attention(self.qkv[:, :HG], self.cache, self.table, self.kv_len, max_kv=self.table.shape[1] * self.T, workspace=self.ws)
+
+
+@gpu
+def test_a_layer_step_by_step():
+    """Every stage of a decode loop against 64 bits on what the stage before it left."""
+    L = Layer()
+    kept = [[], []]
+    for step in range(20):
+        L.x = L.x.roll(step, 1)
+        L.step()
+        act = mxp.dequantize(L.act, mxp.MXFP8).double().cpu()
+        qw = mxp.dequantize(L.qw, mxp.MXFP4P).double().cpu()
+        y = (act @ qw.T).view(L.n, -1, L.D)
+        got = L.qkv.double().cpu()
+        assert ((got - y).abs() <= 2.0 ** -8 * y.abs() + 2.0 ** -15 * (act.abs() @ qw.abs().T).view_as(y)).all()
+        HG = L.H * L.G
+        for part, rows in ((0, got[:, HG:HG + L.H]), (1, got[:, HG + L.H:])):
+            b = np.ascontiguousarray(rows.float().numpy()).reshape(-1, L.D)
+            kept[part].append(oracle.dequantize(oracle.quantize(b, oracle.MXFP4P), oracle.MXFP4P).reshape(L.n, L.H, L.D))
+        k, v = (np.stack(x, 1).repeat(L.G, 2) for x in kept)                 # [n][t][heads][D]
+        q = got[:, :HG].numpy()
+        z = np.einsum("nhd,nthd->nht", q, k) * L.D ** -0.5
+        p = np.exp(z - z.max(-1, keepdims=True))
+        p /= p.sum(-1, keepdims=True)
+        o, S = np.einsum("nht,nthd->nhd", p, v), np.einsum("nht,nthd->nhd", p, abs(v))
+        size = np.einsum("nhd,nthd->nht", abs(q), abs(k)).max() * L.D ** -0.5
+        tol = (4 * (L.D + 8) * 2.0 ** -24 * size + 2.0 ** -8 + 100 * 2.0 ** -24) * S + 2.0 ** -8 * abs(o)
+        assert (abs(L.o.double().cpu().numpy() - o) <= tol).all()
+
+
+@gpu
+@pytest.mark.parametrize("own_stream", [False, True])
+def test_a_layer_captured_and_replayed(own_stream):
+    """The step in a HIP graph: every replay, with eager work and new inputs in between, against the eager step on a twin."""
+    L, E = Layer(), Layer()
+    L.step(); E.step()                                            # (first calls set launch attributes)
+    L.kv_len.zero_(); E.kv_len.zero_()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        L.step()
+    L.kv_len.zero_()
+    side = torch.cuda.Stream()
+    for step in range(6):
+        new = torch.randn(L.x.shape, generator=torch.Generator().manual_seed(step)).bfloat16().cuda()
+        L.x.copy_(new); E.x.copy_(new)
+        graph.replay()
+        if own_stream:                                            # the eager step on a stream of its own
+            side.wait_stream(torch.cuda.current_stream())
+            with torch.cuda.stream(side):
+                E.step()
+            torch.cuda.current_stream().wait_stream(side)
+        else:
+            E.step()
+        torch.cuda.synchronize()
+        assert torch.equal(L.o, E.o) and torch.equal(L.h, E.h) and torch.equal(L.kv_len, E.kv_len)
+        torch.randn(1000, device="cuda").sum().item()
+
+
+@gpu
+def test_two_streams_with_workspaces_of_their_own():
+    """Split sequences on two streams at once: each call's parts lie in its own workspace."""
+    b = [Batch("MXFP4P", 64, 2, 4, 128, [4000, 900], [1, 1], seed=s) for s in (1, 2)]
+    caches = [x.cache() for x in b]
+    want = [x.call(c) for x, c in zip(b, caches)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in b]
+    for _ in range(5):
+        got = []
+        for x, c, s in zip(b, caches, streams):
+            with torch.cuda.stream(s):
+                got.append(x.call(c))
+        torch.cuda.synchronize()
+        assert all(torch.equal(g, w) for gs, ws in zip(got, want) for g, w in zip(gs, ws))
