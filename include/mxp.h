@@ -391,8 +391,8 @@ int mxp_cache_read(const void* cache, int64_t n_pages, int64_t page_tokens, int6
  * A row that sees nothing gets O = 0 and lse = -infinity.  What an invisible token's slot holds, a NaN block included, has no
  * influence; a visible NaN block makes the scores (keys) or the 32 outputs (values) it meets NaN.
  * Q is MXP_BF16 (MXP_F32: MXP_ERR_UNSUPPORTED); keys and values are de-converted by Eq. 2 (exact) inside the kernel and multiplied
- * on the bf16 MFMA; scores, softmax and sums are fp32.  For fp32 O the weights p enter the second product as two bf16 terms
- * (to 2^-16 of each), for bf16 O as one (to 2^-8).  Values below 2^-126 may count as zero.  lse [rows][heads] fp32 may be NULL.
+ * on the bf16 MFMA; scores, softmax and sums are fp32.  For fp32 O the weights p enter the second product as three
+ * bf16 terms (all their bits), for bf16 O as one (to 2^-8).  Values below 2^-126 may count as zero.  lse [rows][heads] fp32 may be NULL.
  * kv_len, table and q_start are read on the device only.  max_q and max_kv are the caller's upper bounds on queries and kv_len of a
  * sequence: they choose launch and splitting, larger sequences are computed all the same, more slowly.
  * rows * heads is at most 2^30 (else MXP_ERR_UNSUPPORTED).

@@ -42,7 +42,8 @@ struct AttnArgs {
   const int32_t *q_start, *kv_len, *table;
   int64_t ld_table;
   int n_seq, heads, group, causal, window;                   // group: query heads per key-value head; window 0: none
-  float scale;                                               // scale * log2(e)
+  float scale;                                               // |scale| * log2(e), at least the smallest normal number
+  uint32_t flip;                                             // sign bits of two bf16 where scale is negative: Q is negated
   const uint8_t* data;
   CacheGeom g;
   void* o;
@@ -80,6 +81,27 @@ __device__ __forceinline__ uint32_t bf16_pair(float a, float b) {   // rounded t
 }
 
 constexpr int64_t kMostTokens = (int64_t)1 << 30, kMostRows = (int64_t)1 << 30;   // per sequence; rows x heads of a call
+
+// Eight weights of one row, 2^(scale x - base), as the bf16 terms of an operand; their sum.  A term is the rounded rest that the
+// terms before it leave: three hold all 24 bits.
+template <int TERMS>
+__device__ __forceinline__ float weights(f32x4 x0, f32x4 x1, float scale, float base, Operand (&p)[TERMS]) {
+  float e[8], sum = 0.0f;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) e[j] = exp2_of(__builtin_fmaf(j < 4 ? x0[j & 3] : x1[j & 3], scale, -base));
+#pragma unroll
+  for (int j = 0; j < 8; j += 2) sum += e[j] + e[j + 1];
+#pragma unroll
+  for (int c = 0; c < TERMS; ++c)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const uint32_t u = bf16_pair(e[2 * j], e[2 * j + 1]);
+      p[c].u[j] = u;
+      e[2 * j] -= __uint_as_float(u << 16);
+      e[2 * j + 1] -= __uint_as_float(u & 0xFFFF0000u);
+    }
+  return sum;
+}
 
 // ---- one sequence's share of the work -------------------------------------------------------------------------------
 struct Sequence {
@@ -122,15 +144,18 @@ struct Span {
   }
 };
 
-// The page of a token: its record of this head's keys, and whether there is one
+// The page of a token: its number, or -1 where it has none
+__device__ __forceinline__ int32_t page_of(const AttnArgs& a, const Sequence& s, int64_t t) {
+  const int64_t j = t >> a.g.page_shift;
+  const int32_t p = j < a.ld_table ? s.pages[j] : -1;
+  return p < a.g.n_pages ? p : -1;
+}
 struct Page {
-  const uint8_t* rec;
+  const uint8_t* rec;                                        // its record of this head's keys (page 0's if there is none)
   int at;                                                    // the token's place in it
   bool held;
-  __device__ __forceinline__ Page(const AttnArgs& a, const Sequence& s, int head, int t) {
-    const int64_t j = t >> a.g.page_shift;
-    const int32_t p = j < a.ld_table ? s.pages[j] : -1;
-    held = p >= 0 && p < a.g.n_pages;
+  __device__ __forceinline__ Page(const AttnArgs& a, int head, int32_t p, int t) {
+    held = p >= 0;
     rec = a.data + ((int64_t)(held ? p : 0) * a.g.kv_heads + head) * 2 * a.g.part_bytes;
     at = t & ((1 << a.g.page_shift) - 1);
   }
@@ -173,8 +198,8 @@ __device__ __forceinline__ void expand(const Block& b, bool drop, uint8_t* dst) 
     const uint32_t pos = b.index & 31u;
     const uint32_t lo = pos & 8u ? b.code[1] : b.code[0], hi = pos & 8u ? b.code[3] : b.code[2];
     const uint32_t nib = ((pos & 16u ? hi : lo) >> (4u * (pos & 7u))) & 15u;
-    const uint32_t h = b.scale == 255u ? 0x7FC0u : ((nib & 8u) << 12) | ((b.scale + 2u) << 7) | ((nib & 7u) << 4);
-    reinterpret_cast<u16a*>(dst)[pos] = (uint16_t)(zero ? 0u : h);
+    const uint32_t h = (((nib & 8u) << 12) | ((b.scale + 2u) << 7) | ((nib & 7u) << 4)) & keep;   // (scale byte 255: any number among NaN)
+    reinterpret_cast<u16a*>(dst)[pos] = (uint16_t)h;
   }
 }
 
@@ -224,21 +249,27 @@ constexpr int kFewWaves = 4;
 template <int D>
 constexpr int few_pitch() { return 2 * D + 16; }             // bytes per token: 16 rows' 16-byte reads fall on all banks
 template <int D>
-constexpr int few_lds(int nt) { return kFewWaves * (2 * 32 * few_pitch<D>() + 16 * nt * 8); }
+constexpr int few_patch(int nt) { return 32 * few_pitch<D>() > 16 * nt * D * 4 ? 32 * few_pitch<D>() : 16 * nt * D * 4; }
+template <int D>
+constexpr int few_lds(int nt) { return kFewWaves * (few_patch<D>(nt) + 16 * nt * 8); }
+constexpr int few_waves_per_simd(int D, int NT) { return D * NT <= 128 ? 4 : D * NT <= 256 ? 2 : 1; }
 
 // NT tiles of 16 rows; TERMS: bf16 terms of P
 template <int D, int MODE, int NT, int TERMS>
-__global__ void __launch_bounds__(64 * kFewWaves) attn_few_kernel(const AttnArgs a) {
-  constexpr int DB = D / 32, NB = D / 64, PITCH = few_pitch<D>();   // blocks per token; blocks per lane of a 32-token tile
+__global__ void __launch_bounds__(64 * kFewWaves, few_waves_per_simd(D, NT)) attn_few_kernel(const AttnArgs a) {
+  constexpr int DB = D / 32, NB = D / 64, PITCH = few_pitch<D>(), PATCH = few_patch<D>(NT);   // blocks per token; per lane of a 32-token tile
+  constexpr int LANE_TOKENS = D == 64 ? 32 : 16;             // tokens that a wavefront's lanes cover with one block each (of 2, 4, 4 neighbours)
   extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 15, quarter = lane >> 4;
-  uint8_t* const kt = lds + wave * 2 * 32 * PITCH;
-  uint8_t* const vt = kt + 32 * PITCH;
-  float* const ml = reinterpret_cast<float*>(lds + kFewWaves * 2 * 32 * PITCH);   // [wave][row][2]
+  uint8_t* const patch = lds + wave * PATCH;                 // a tile's keys, then its values
+  float* const ml = reinterpret_cast<float*>(lds + kFewWaves * PATCH);   // [wave][row][2]
   const Work w(a);
   const Sequence s(a, w.seq);
   const int R = s.n * a.group;
+  // this lane's blocks of a tile: its token (16 lanes in a row have 16 tokens: their stores fall on all banks), its block of the token
+  const auto token_of = [&](int i) { return D == 256 ? 16 * (i >> 1) + (lane & 15) : LANE_TOKENS * i + (lane & (LANE_TOKENS - 1)); };
+  const auto block_of = [&](int i) { return D == 256 ? 4 * (i & 1) + (lane >> 4) : lane / LANE_TOKENS; };
   for (int r0 = w.tile * 16 * NT; r0 < R; r0 += a.row_tiles * 16 * NT) {
     const Span span(a, s, r0, R - r0 < 16 * NT ? R - r0 : 16 * NT, w.split);
     // this lane's rows, as operands of the first product: channels 32 st + 8 quarter ... + 7
@@ -255,7 +286,7 @@ __global__ void __launch_bounds__(64 * kFewWaves) attn_few_kernel(const AttnArgs
       for (int st = 0; st < DB; ++st) {
         const u32x4 x = *reinterpret_cast<const u32x4*>(p + 32 * st);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) q[t][st].u[j] = there ? x[j] : 0u;
+        for (int j = 0; j < 4; ++j) q[t][st].u[j] = there ? x[j] ^ a.flip : 0u;
       }
     }
     // tokens that every row of the tile sees
@@ -269,92 +300,94 @@ __global__ void __launch_bounds__(64 * kFewWaves) attn_few_kernel(const AttnArgs
 #pragma unroll
       for (int d = 0; d < D / 16; ++d) o[t][d] = f32x4{0, 0, 0, 0};
     }
+    // The wavefront's tiles: span.begin + 32 wave, and every 32 kFewWaves tokens from there.  Lane n holds the page of half n % 2 of
+    // tile n / 2 of the next 32 tiles (-1: none), so that a tile's addresses wait for no table.
+    const int begin = span.begin + 32 * wave;
+    int tile = 0;
+    int32_t pages = -1;
     Block kb[NB], vb[NB];
     bool held0 = false, held1 = false;                       // whether the tile's two halves have a page
     const auto fetch = [&](int t) {
-      const Page p0(a, s, w.head, t), p1(a, s, w.head, t + 16);
+      if ((tile & 31) == 0) pages = page_of(a, s, (int64_t)t + 32 * kFewWaves * (lane >> 1) + 16 * (lane & 1));
+      const Page p0(a, w.head, __builtin_amdgcn_readlane(pages, 2 * (tile & 31)), t), p1(a, w.head, __builtin_amdgcn_readlane(pages, 2 * (tile & 31) + 1), t + 16);
       held0 = p0.held;
       held1 = p1.held;
+      ++tile;
 #pragma unroll
       for (int i = 0; i < NB; ++i) {
-        const int n = lane + 64 * i, token = n / DB;
-        const bool second = NB == 1 ? token >= 16 : i >= NB / 2;
+        const int token = token_of(i);
+        const bool second = D == 64 ? token >= 16 : i >= NB / 2;
         const uint8_t* rec = second ? p1.rec : p0.rec;
-        const int row = second ? p1.at + token - 16 : p0.at + token;
-        kb[i] = load_block<D, MODE>(rec, a.g, row, n % DB);
-        vb[i] = load_block<D, MODE>(rec + a.g.part_bytes, a.g, row, n % DB);
+        const int row = second ? p1.at + (token & 15) : p0.at + token;
+        kb[i] = load_block<D, MODE>(rec, a.g, row, block_of(i));
+        vb[i] = load_block<D, MODE>(rec + a.g.part_bytes, a.g, row, block_of(i));
       }
     };
-    int t0 = span.begin + 32 * wave;
-    if (t0 < span.end) fetch(t0);
-    for (; t0 < span.end; t0 += 32 * kFewWaves) {
+    if (begin < span.end) fetch(begin);
+    for (int t0 = begin; t0 < span.end; t0 += 32 * kFewWaves) {
       const bool h0 = held0, h1 = held1;
       uint64_t nan[NB];                                      // lanes whose block of V is NaN: zeros here, put in behind the product
       uint64_t any = 0;
 #pragma unroll
-      for (int i = 0; i < NB; ++i) {
-        const int n = lane + 64 * i, token = n / DB;
-        const bool dead = t0 + token >= span.end || !(token >= 16 ? h1 : h0);
-        expand<MODE>(kb[i], false, kt + token * PITCH + (n % DB) * 64);
-        nan[i] = __ballot(vb[i].scale == 255u && !dead);
-        any |= nan[i];
-        expand<MODE>(vb[i], dead || vb[i].scale == 255u, vt + token * PITCH + (n % DB) * 64);
-      }
+      for (int i = 0; i < NB; ++i) expand<MODE>(kb[i], false, patch + token_of(i) * PITCH + block_of(i) * 64);
       __builtin_amdgcn_wave_barrier();
-      if (t0 + 32 * kFewWaves < span.end) fetch(t0 + 32 * kFewWaves);
       f32x4 sc[NT][2];
 #pragma unroll
-      for (int t = 0; t < NT; ++t) sc[t][0] = sc[t][1] = f32x4{0, 0, 0, 0};
+      for (int h = 0; h < 2; ++h) {
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
+        for (int t = 0; t < NT; ++t) sc[t][h] = f32x4{0, 0, 0, 0};
 #pragma unroll
         for (int st = 0; st < DB; ++st) {
           Operand k;
-          const u32x4 x = *reinterpret_cast<const u32x4*>(kt + (16 * h + col) * PITCH + (32 * st + 8 * quarter) * 2);
+          const u32x4 x = *reinterpret_cast<const u32x4*>(patch + (16 * h + col) * PITCH + (32 * st + 8 * quarter) * 2);
 #pragma unroll
           for (int j = 0; j < 4; ++j) k.u[j] = x[j];
 #pragma unroll
           for (int t = 0; t < NT; ++t) sc[t][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k.v, q[t][st].v, sc[t][h], 0, 0, 0);
         }
+      }
+      __builtin_amdgcn_wave_barrier();                       // (the reads above come first: LDS serves a wavefront in order)
+#pragma unroll
+      for (int i = 0; i < NB; ++i) {
+        const int token = token_of(i);
+        const bool dead = t0 + token >= span.end || !(token >= 16 ? h1 : h0);
+        nan[i] = __ballot(vb[i].scale == 255u && !dead);
+        any |= nan[i];
+        expand<MODE>(vb[i], dead || vb[i].scale == 255u, patch + token * PITCH + block_of(i) * 64);
+      }
+      __builtin_amdgcn_wave_barrier();
+      if (t0 + 32 * kFewWaves < span.end) fetch(t0 + 32 * kFewWaves);
       const bool whole = h0 && h1 && t0 >= all_from && t0 + 31 <= all_to && t0 + 32 <= span.end;   // (uniform)
+      if (!whole) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const int tok = t0 + 16 * h + 4 * quarter + i;
+              sc[t][h][i] = tok >= first[t] && tok <= last[t] && tok < span.end && (h ? h1 : h0) ? sc[t][h][i] : -kInf;
+            }
+      }
       Operand p[NT][TERMS];
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
-        float x[8], mx = -kInf;
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            float y = sc[t][h][i] * a.scale;
-            if (!whole) {
-              const int tok = t0 + 16 * h + 4 * quarter + i;
-              y = tok >= first[t] && tok <= last[t] && tok < span.end && (h ? h1 : h0) ? y : -kInf;
-            }
-            x[4 * h + i] = y;
-            mx = fmaxf(mx, y);
-          }
+        float mx = fmaxf(fmaxf(fmaxf(sc[t][0][0], sc[t][0][1]), fmaxf(sc[t][0][2], sc[t][0][3])), fmaxf(fmaxf(sc[t][1][0], sc[t][1][1]), fmaxf(sc[t][1][2], sc[t][1][3])));
         mx = fmaxf(m[t], max_across_32(max_across_16(mx)));
-        const float base = zero_if_none(mx);
+        const float base = zero_if_none(mx) * a.scale;
         if (__any(mx != m[t])) {
-          const float f = exp2_of(m[t] - base);
+          const float f = exp2_of(m[t] * a.scale - base);
           l[t] *= f;
 #pragma unroll
           for (int d = 0; d < D / 16; ++d) o[t][d] *= f;
           m[t] = mx;
         }
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const float e0 = exp2_of(x[2 * j] - base), e1 = exp2_of(x[2 * j + 1] - base);
-          l[t] += e0 + e1;
-          p[t][0].u[j] = bf16_pair(e0, e1);
-          if (TERMS == 2)
-            p[t][TERMS - 1].u[j] = bf16_pair(e0 - __uint_as_float(p[t][0].u[j] << 16), e1 - __uint_as_float(p[t][0].u[j] & 0xFFFF0000u));
-        }
+        l[t] += weights<TERMS>(sc[t][0], sc[t][1], a.scale, base, p[t]);
       }
 #pragma unroll
       for (int d = 0; d < D / 16; ++d) {
         Operand v;
-        const uint8_t* at = vt + (4 * quarter + (col >> 2)) * PITCH + (16 * d + 4 * (col & 3)) * 2;
+        const uint8_t* at = patch + (4 * quarter + (col >> 2)) * PITCH + (16 * d + 4 * (col & 3)) * 2;
         v.s[0] = read_transposed(at);
         v.s[1] = read_transposed(at + 16 * PITCH);
 #pragma unroll
@@ -366,26 +399,25 @@ __global__ void __launch_bounds__(64 * kFewWaves) attn_few_kernel(const AttnArgs
 #pragma unroll
         for (int i = 0; i < NB; ++i)
           for (uint64_t left = nan[i]; left; left &= left - 1) {
-            const int n = __builtin_ctzll(left) + 64 * i, tok = t0 + n / DB;
+            const int who = __builtin_ctzll(left), tok = t0 + __builtin_amdgcn_readlane(token_of(i), who), blk = __builtin_amdgcn_readlane(block_of(i), who);
 #pragma unroll
             for (int t = 0; t < NT; ++t)
               if (tok >= first[t] && tok <= last[t]) {
 #pragma unroll
                 for (int d = 0; d < D / 16; ++d)
-                  if (d / 2 == n % DB) o[t][d] = f32x4{1, 1, 1, 1} * __uint_as_float(0x7FC00000u);
+                  if (d / 2 == blk) o[t][d] = f32x4{1, 1, 1, 1} * __uint_as_float(0x7FC00000u);
               }
           }
       }
       __builtin_amdgcn_wave_barrier();
     }
     // join the wavefronts: each leaves its rows in its own patch
-    __syncthreads();
-    float* const mine = reinterpret_cast<float*>(kt);
+    float* const mine = reinterpret_cast<float*>(patch);
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
       const float sum = sum_across_32(sum_across_16(l[t]));
       if (quarter == 0) {
-        ml[(wave * 16 * NT + 16 * t + col) * 2] = m[t];
+        ml[(wave * 16 * NT + 16 * t + col) * 2] = m[t] * a.scale;
         ml[(wave * 16 * NT + 16 * t + col) * 2 + 1] = sum;
       }
 #pragma unroll
@@ -404,7 +436,7 @@ __global__ void __launch_bounds__(64 * kFewWaves) attn_few_kernel(const AttnArgs
       for (int v = 0; v < kFewWaves; ++v) {
         const float f = exp2_of(ml[(v * 16 * NT + row) * 2] - base);
         sum += ml[(v * 16 * NT + row) * 2 + 1] * f;
-        out += *reinterpret_cast<const f32x4*>(lds + v * 2 * 32 * PITCH + (row * D + d) * 4) * f;
+        out += *reinterpret_cast<const f32x4*>(lds + v * PATCH + (row * D + d) * 4) * f;
       }
       const int i = r / a.group, head = w.head * a.group + r - i * a.group;
       finish_values(a, w.split, s.q0 + i, head, d, out, sum);
@@ -450,7 +482,7 @@ __global__ void __launch_bounds__(64 * kManyWaves) attn_many_kernel(const AttnAr
       for (int st = 0; st < D / 16; ++st) {
         const u32x4 x = *reinterpret_cast<const u32x4*>(p + 16 * st);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) q[st].u[j] = there ? x[j] : 0u;
+        for (int j = 0; j < 4; ++j) q[st].u[j] = there ? x[j] ^ a.flip : 0u;
       }
     }
     // what the wavefront's rows see: some of them, all of them
@@ -466,17 +498,21 @@ __global__ void __launch_bounds__(64 * kManyWaves) attn_many_kernel(const AttnAr
       for (int j = 0; j < 16; ++j) o[d][j] = 0.0f;
     Block kb[NL], vb[NL];
     uint32_t held = 0, held_next = 0;                        // bit j: tokens 16 j ... + 15 of the tile have a page
+    int tile = 0;
+    int32_t pages = -1;                                      // lane n: the page of tokens 16 (n % 4) ... of tile n / 4 of the next 16
     const auto fetch = [&](int t) {
+      if ((tile & 15) == 0) pages = page_of(a, s, (int64_t)t + 16 * lane);
       held_next = 0;
       const uint8_t* rec[4];
       int at[4];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const Page p(a, s, w.head, t + 16 * j);
+        const Page p(a, w.head, __builtin_amdgcn_readlane(pages, 4 * (tile & 15) + j), t + 16 * j);
         held_next |= (p.held ? 1u : 0u) << j;
         rec[j] = p.rec;
         at[j] = p.at;
       }
+      ++tile;
 #pragma unroll
       for (int k = 0; k < NL; ++k) {
         const int n = (int)threadIdx.x + 64 * kManyWaves * k, token = n / DB;
@@ -533,23 +569,24 @@ __global__ void __launch_bounds__(64 * kManyWaves) attn_many_kernel(const AttnAr
           }
         }
         const bool whole = held == 15u && t0 >= all_from && t0 + kManyTokens - 1 <= all_to && t0 + kManyTokens <= span.end;
+        if (!whole) {
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+              const int tok = t0 + 32 * h + 8 * (j >> 2) + 4 * half + (j & 3);
+              sc[h][j] = tok >= first && tok <= last && tok < span.end && ((held >> (2 * h + (j >> 3))) & 1u) ? sc[h][j] : -kInf;
+            }
+        }
         float mx = -kInf;
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
-          for (int j = 0; j < 16; ++j) {
-            float y = sc[h][j] * a.scale;
-            if (!whole) {
-              const int in = 32 * h + 8 * (j >> 2) + 4 * half + (j & 3), tok = t0 + in;
-              y = tok >= first && tok <= last && tok < span.end && ((held >> (2 * h + (j >> 3))) & 1u) ? y : -kInf;
-            }
-            sc[h][j] = y;
-            mx = fmaxf(mx, y);
-          }
+          for (int j = 0; j < 16; ++j) mx = fmaxf(mx, sc[h][j]);
         mx = fmaxf(m, max_across_32(mx));
-        const float base = zero_if_none(mx);
+        const float base = zero_if_none(mx) * a.scale;
         if (__any(mx != m)) {
-          const float f = exp2_of(m - base);
+          const float f = exp2_of(m * a.scale - base);
           l *= f;
 #pragma unroll
           for (int d = 0; d < DB; ++d) o[d] *= f;
@@ -558,13 +595,9 @@ __global__ void __launch_bounds__(64 * kManyWaves) attn_many_kernel(const AttnAr
 #pragma unroll
         for (int b = 0; b < 4; ++b) {                        // 16 tokens: registers 8 (b % 2) ... + 7 of half b / 2
           Operand p[TERMS];
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const float e0 = exp2_of(sc[b >> 1][8 * (b & 1) + 2 * j] - base), e1 = exp2_of(sc[b >> 1][8 * (b & 1) + 2 * j + 1] - base);
-            l += e0 + e1;
-            p[0].u[j] = bf16_pair(e0, e1);
-            if (TERMS == 2) p[TERMS - 1].u[j] = bf16_pair(e0 - __uint_as_float(p[0].u[j] << 16), e1 - __uint_as_float(p[0].u[j] & 0xFFFF0000u));
-          }
+          const int j = 8 * (b & 1);
+          const f32x16& x = sc[b >> 1];
+          l += weights<TERMS>(f32x4{x[j], x[j + 1], x[j + 2], x[j + 3]}, f32x4{x[j + 4], x[j + 5], x[j + 6], x[j + 7]}, a.scale, base, p);
 #pragma unroll
           for (int d = 0; d < DB; ++d) {
             Operand v;
@@ -605,36 +638,59 @@ __global__ void __launch_bounds__(64 * kManyWaves) attn_many_kernel(const AttnAr
 #pragma unroll
         for (int j = 0; j < 4; ++j)
           finish_values(a, w.split, s.q0 + i, head, 32 * d + 8 * j + 4 * half, f32x4{o[d][4 * j], o[d][4 * j + 1], o[d][4 * j + 2], o[d][4 * j + 3]}, l);
-      if (half == 0) finish_row(a, w.split, s.q0 + i, head, m, l);
+      if (half == 0) finish_row(a, w.split, s.q0 + i, head, m * a.scale, l);
     }
     __syncthreads();
   }
 }
 
 // ---- the parts of split sequences ---------------------------------------------------------------------------------------
-// A wavefront per (row, head): the parts' maxima and sums, then the values of the parts that saw anything.  Rows that no
-// sequence has are left as they are.
+// A workgroup per (row, head): every lane the weight of one part (at most kMostSplits = lanes), then D / 4 lanes across a row and
+// 1024 / D parts at a time.  Rows that no sequence has are left as they are.
+constexpr int kMostSplits = 256;
 __global__ void __launch_bounds__(256) attn_join_kernel(const AttnArgs a) {
-  const int lane = threadIdx.x & 63;
+  __shared__ float weight[kMostSplits], top_of[4], sum_of[4];
+  __shared__ __attribute__((aligned(16))) float acc[1024];
+  const int t = threadIdx.x, across = a.g.D >> 2, d = 4 * (t & (across - 1)), g = t / across, groups = 256 / across;
   const int64_t from = a.q_start ? a.q_start[0] : 0, to = a.q_start ? a.q_start[a.n_seq] : a.rows, n = a.rows * a.heads;
-  for (int64_t j = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); j < n; j += (int64_t)gridDim.x * 4) {
+  for (int64_t j = blockIdx.x; j < n; j += gridDim.x) {
     const int64_t row = j / a.heads;
-    if (row < from || row >= to) continue;
+    if (row < from || row >= to) continue;                   // (the whole workgroup)
     const int head = (int)(j - row * a.heads);
-    float top = -kInf;
-    for (int p = 0; p < a.splits; ++p) top = fmaxf(top, a.part_ml[(p * n + j) * 2]);
-    const float base = zero_if_none(top);
-    float sum = 0.0f;
-    f32x4 out = {0, 0, 0, 0};
-    for (int p = 0; p < a.splits; ++p) {
-      const float lp = a.part_ml[(p * n + j) * 2 + 1];
-      if (lp == 0.0f) continue;
-      const float f = exp2_of(a.part_ml[(p * n + j) * 2] - base);
-      sum += lp * f;
-      if (4 * lane < a.g.D) out += *reinterpret_cast<const f32x4*>(a.part_o + (p * n + j) * a.g.D + 4 * lane) * f;
+    float m = -kInf, l = 0.0f;
+    if (t < a.splits) {
+      m = a.part_ml[(t * n + j) * 2];
+      l = a.part_ml[(t * n + j) * 2 + 1];
     }
-    if (4 * lane < a.g.D) store_out(a, row, head, 4 * lane, sum == 0.0f ? f32x4{0, 0, 0, 0} : out / sum);
-    if (lane == 0 && a.lse) a.lse[row * a.heads + head] = lse_of(top, sum);
+    float top = m;
+#pragma unroll
+    for (int x = 32; x >= 1; x >>= 1) top = fmaxf(top, __shfl_xor(top, x));
+    if ((t & 63) == 0) top_of[t >> 6] = top;
+    __syncthreads();
+    top = fmaxf(fmaxf(top_of[0], top_of[1]), fmaxf(top_of[2], top_of[3]));
+    const float f = l == 0.0f ? 0.0f : exp2_of(m - zero_if_none(top));   // (0: a part that saw nothing, left out below)
+    weight[t] = f;
+    float sum = l * f;
+#pragma unroll
+    for (int x = 32; x >= 1; x >>= 1) sum += __shfl_xor(sum, x);
+    if ((t & 63) == 0) sum_of[t >> 6] = sum;
+    __syncthreads();
+    sum = (sum_of[0] + sum_of[1]) + (sum_of[2] + sum_of[3]);
+    f32x4 out = {0, 0, 0, 0};
+#pragma unroll 4
+    for (int p = g; p < a.splits; p += groups) {
+      const float w = weight[p];
+      const f32x4 x = *reinterpret_cast<const f32x4*>(a.part_o + (p * n + j) * a.g.D + d);
+      if (w != 0.0f) out += x * w;
+    }
+    *reinterpret_cast<f32x4*>(acc + 4 * t) = out;
+    __syncthreads();
+    if (g == 0) {
+      for (int p = 1; p < groups; ++p) out += *reinterpret_cast<const f32x4*>(acc + 4 * (t + p * across));
+      store_out(a, row, head, d, sum == 0.0f ? f32x4{0, 0, 0, 0} : out / sum);
+    }
+    if (t == 0 && a.lse) a.lse[row * a.heads + head] = lse_of(top, sum);
+    __syncthreads();
   }
 }
 
@@ -662,7 +718,7 @@ Plan plan_for(int64_t n_seq, int64_t max_q, int64_t max_kv, int64_t heads, int64
   int64_t splits = base < want ? (want + base - 1) / base : 1;
   if (splits > (len + least - 1) / least) splits = (len + least - 1) / least;
   if (splits < 1) splits = 1;
-  if (splits > 256) splits = 256;
+  if (splits > kMostSplits) splits = kMostSplits;
   const int64_t step = p.many ? kManyTokens : 32 * kFewWaves;
   const int64_t chunk = ((len + splits - 1) / splits + step - 1) / step * step;
   p.chunk = (int)(chunk < step ? step : chunk > (1 << 30) ? (1 << 30) : chunk);
@@ -742,7 +798,9 @@ extern "C" int mxp_attention(const void* Q, int q_dtype, int64_t ld_q, int64_t r
   a.group = (int)(heads / kv_heads);
   a.causal = causal ? 1 : 0;
   a.window = (int)(window < 2147483647LL ? window : 2147483647LL);
-  a.scale = scale * 1.4426950408889634f;
+  a.scale = (scale < 0 ? -scale : scale) * 1.4426950408889634f;
+  if (a.scale < 1.17549435e-38f) a.scale = 1.17549435e-38f;   // (0 would make NaN of a hidden token's -infinity)
+  a.flip = scale < 0 ? 0x80008000u : 0u;
   a.data = static_cast<const uint8_t*>(cache);
   a.o = O;
   a.ld_o = ld_o;
@@ -754,7 +812,7 @@ extern "C" int mxp_attention(const void* Q, int q_dtype, int64_t ld_q, int64_t r
   a.chunk = p.chunk;
   a.row_tiles = p.row_tiles;
   hipStream_t s = static_cast<hipStream_t>(stream);
-#define MXP_ATTN_T(D, M) do { if (a.o_bf16) launch<D, M, 1>(a, p, s); else launch<D, M, 2>(a, p, s); } while (0)
+#define MXP_ATTN_T(D, M) do { if (a.o_bf16) launch<D, M, 1>(a, p, s); else launch<D, M, 3>(a, p, s); } while (0)
 #define MXP_ATTN_M(D) do { if (fmt == MXP_FMT_MXFP4) MXP_ATTN_T(D, 0); else if (fmt == MXP_FMT_MXFP4P) MXP_ATTN_T(D, 1); else MXP_ATTN_T(D, 2); } while (0)
   if (head_dim == 64) MXP_ATTN_M(64);
   else if (head_dim == 128) MXP_ATTN_M(128);
@@ -762,7 +820,7 @@ extern "C" int mxp_attention(const void* Q, int q_dtype, int64_t ld_q, int64_t r
 #undef MXP_ATTN_M
 #undef MXP_ATTN_T
   if (p.splits > 1) {
-    const int64_t want = (rows * heads + 3) / 4;
+    const int64_t want = rows * heads;
     hipLaunchKernelGGL(attn_join_kernel, dim3((unsigned)(want < (1 << 20) ? want : (1 << 20))), dim3(256), 0, s, a);
   }
   return launch_status();

@@ -259,11 +259,11 @@ class Batch:
         """Against 64 bits.  An output is off by at most
             2 e S + p S + a S + u |o|,    S = sum p |v| / sum p,
         e: a score's error, 2 (D + 8) 2^-24 of the largest visible scale * sum |q k| (the product's sums and the roundings behind it),
-        once in p and once in the sum; p: the rounding of p to one bf16 term (2^-8, bf16 output) or two (2^-16); a: fp32 sums over the
+        once in p and once in the sum; p: the rounding of p to one bf16 term (2^-8, bf16 output) or three (2^-24); a: fp32 sums over the
         tokens and joins, (tokens + 64) 2^-24, exp2 and the division in the 64; u: the output's own rounding."""
         scale = self.D ** -0.5 if scale is None else scale
         got, got_lse, qh = out.double().cpu().numpy(), lse.double().cpu().numpy(), self.q.double().cpu().numpy()
-        p_err, u = (2.0 ** -8, U[torch.bfloat16]) if out.dtype == torch.bfloat16 else (2.0 ** -16, U[torch.float32])
+        p_err, u = (2.0 ** -8, U[torch.bfloat16]) if out.dtype == torch.bfloat16 else (2.0 ** -24, U[torch.float32])
         for s, n in enumerate(self.kv):
             m, rows = self.nq[s], slice(int(self.start[s]), int(self.start[s + 1]))
             k, v = (x[self.slots[s]].transpose(1, 0, 2) for x in self.val)         # [H][n][D]
