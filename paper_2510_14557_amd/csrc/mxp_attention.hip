@@ -14,7 +14,7 @@
 // Query rows of one key-value head (heads that share it x queries) are taken together.  attn_few_kernel: up to 32 of them per
 // workgroup, every wavefront with tokens of its own, joined through LDS at the end; bound by reading the cache.
 // attn_many_kernel: 128 rows per workgroup, the wavefronts share the de-converted tokens; bound by the matrix cores and the softmax.
-// Both can split a sequence's tokens over workgroups; attn_join_kernel then adds the parts.
+// Both can split a sequence's tokens over workgroups; a second kernel then joins the parts.
 #include "mxp_cache.h"
 
 namespace {
@@ -49,8 +49,9 @@ struct AttnArgs {
   void* o;
   int64_t ld_o;
   int o_bf16;
-  float *lse, *part_o, *part_ml;                             // parts: [split][row][head][D], [split][row][head][2]
-  int splits, chunk, row_tiles;
+  float *lse, *part_o, *part_ml;                             // parts of rows: D values, maximum and sum
+  int32_t* joins;                                            // few rows: [workgroup][4], see Share
+  int direct, splits, chunk, row_tiles;
 };
 
 constexpr float kInf = __builtin_inff();
@@ -103,6 +104,12 @@ __device__ __forceinline__ float weights(f32x4 x0, f32x4 x1, float scale, float 
   return sum;
 }
 
+// a value that all lanes have, where the compiler cannot see it
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ int64_t uniform(int64_t x) {
+  return (int64_t)(((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32) | (uint32_t)__builtin_amdgcn_readfirstlane((int)x));
+}
+
 // ---- one sequence's share of the work -------------------------------------------------------------------------------
 struct Sequence {
   int64_t q0;                                                // first row of Q
@@ -134,6 +141,7 @@ struct Sequence {
 // The tokens that a tile of rows and one split go over: [begin, end), begin a multiple of 32
 struct Span {
   int begin, end;
+  __device__ __forceinline__ Span(int b, int e) : begin(b), end(e) {}
   __device__ __forceinline__ Span(const AttnArgs& a, const Sequence& s, int row, int rows, int split) {   // rows > 0
     const int i0 = row / a.group, i1 = (row + rows - 1) / a.group;
     const int hi = s.last(a, i1) + 1, lo = s.first(a, i0) & ~31;
@@ -244,8 +252,111 @@ struct Work {
   }
 };
 
+// ---- joining parts --------------------------------------------------------------------------------------------------
+// One row of one head from its parts, by a workgroup: every lane the weights of some parts, then D / 4 lanes across a row and
+// 1024 / D parts at a time.
+constexpr int kMostParts = 1024;
+struct JoinRoom {
+  float weight[kMostParts], top_of[4], sum_of[4];
+  __attribute__((aligned(16))) float acc[1024];
+};
+template <class PartAt>
+__device__ __forceinline__ void join_row(const AttnArgs& a, JoinRoom& room, int parts, PartAt part_at, int64_t row, int head) {
+  const int t = threadIdx.x, across = a.g.D >> 2, d = 4 * (t & (across - 1)), g = t / across, groups = 256 / across;
+  float m[kMostParts / 256], l[kMostParts / 256], top = -kInf, sum = 0.0f;
+#pragma unroll
+  for (int k = 0; k < kMostParts / 256; ++k) {
+    m[k] = -kInf;
+    l[k] = 0.0f;
+    if (t + 256 * k < parts) {
+      const int64_t at = part_at(t + 256 * k);
+      m[k] = a.part_ml[2 * at];
+      l[k] = a.part_ml[2 * at + 1];
+    }
+    top = fmaxf(top, m[k]);
+  }
+#pragma unroll
+  for (int x = 32; x >= 1; x >>= 1) top = fmaxf(top, __shfl_xor(top, x));
+  if ((t & 63) == 0) room.top_of[t >> 6] = top;
+  __syncthreads();
+  top = fmaxf(fmaxf(room.top_of[0], room.top_of[1]), fmaxf(room.top_of[2], room.top_of[3]));
+#pragma unroll
+  for (int k = 0; k < kMostParts / 256; ++k) {
+    const float f = l[k] == 0.0f ? 0.0f : exp2_of(m[k] - zero_if_none(top));   // (0: a part that saw nothing, left out below)
+    room.weight[t + 256 * k] = f;
+    sum += l[k] * f;
+  }
+#pragma unroll
+  for (int x = 32; x >= 1; x >>= 1) sum += __shfl_xor(sum, x);
+  if ((t & 63) == 0) room.sum_of[t >> 6] = sum;
+  __syncthreads();
+  sum = (room.sum_of[0] + room.sum_of[1]) + (room.sum_of[2] + room.sum_of[3]);
+  f32x4 out = {0, 0, 0, 0};
+  for (int p0 = g; p0 < parts; p0 += 8 * groups) {           // eight loads at a time
+    f32x4 x[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const int p = p0 + k * groups;
+      x[k] = *reinterpret_cast<const f32x4*>(a.part_o + part_at(p < parts ? p : p0) * a.g.D + d);
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const int p = p0 + k * groups;
+      const float w = p < parts ? room.weight[p] : 0.0f;
+      if (w != 0.0f) out += x[k] * w;
+    }
+  }
+  *reinterpret_cast<f32x4*>(room.acc + 4 * t) = out;
+  __syncthreads();
+  if (g == 0) {
+    for (int p = 1; p < groups; ++p) out += *reinterpret_cast<const f32x4*>(room.acc + 4 * (t + p * across));
+    store_out(a, row, head, d, sum == 0.0f ? f32x4{0, 0, 0, 0} : out / sum);
+  }
+  if (t == 0 && a.lse) a.lse[row * a.heads + head] = lse_of(top, sum);
+  __syncthreads();
+}
+
+// The same by a wavefront, for at most 64 parts: a part's weight is a lane's.
+template <class PartAt>
+__device__ __forceinline__ void join_row_by_wave(const AttnArgs& a, int parts, PartAt part_at, int64_t row, int head) {
+  const int lane = threadIdx.x & 63, across = a.g.D >> 2, d = 4 * (lane & (across - 1)), g = lane / across, groups = 64 / across;
+  float m = -kInf, l = 0.0f;
+  if (lane < parts) {
+    const int64_t at = part_at(lane);
+    m = a.part_ml[2 * at];
+    l = a.part_ml[2 * at + 1];
+  }
+  f32x4 x[4];                                                // (on their way before the weights are known)
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const int p = g + k * groups;
+    x[k] = *reinterpret_cast<const f32x4*>(a.part_o + part_at(p < parts ? p : 0) * a.g.D + d);
+  }
+  float top = m;
+#pragma unroll
+  for (int i = 32; i >= 1; i >>= 1) top = fmaxf(top, __shfl_xor(top, i));
+  const float f = l == 0.0f ? 0.0f : exp2_of(m - zero_if_none(top));
+  float sum = l * f;
+#pragma unroll
+  for (int i = 32; i >= 1; i >>= 1) sum += __shfl_xor(sum, i);
+  f32x4 out = {0, 0, 0, 0};
+  for (int p0 = 0; p0 < parts; p0 += 4 * groups) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int p = p0 + g + k * groups;
+      const float w = __shfl(f, p & 63);
+      if (p < parts && w != 0.0f) out += (p0 == 0 ? x[k] : *reinterpret_cast<const f32x4*>(a.part_o + part_at(p) * a.g.D + d)) * w;
+    }
+  }
+  for (int i = across; i < 64; i <<= 1)
+#pragma unroll
+    for (int k = 0; k < 4; ++k) out[k] += __shfl_xor(out[k], i);
+  if (g == 0) store_out(a, row, head, d, sum == 0.0f ? f32x4{0, 0, 0, 0} : out / sum);
+  if (lane == 0 && a.lse) a.lse[row * a.heads + head] = lse_of(top, sum);
+}
+
 // ---- few rows -------------------------------------------------------------------------------------------------------
-constexpr int kFewWaves = 4;
+constexpr int kFewWaves = 4, kFewAhead = 1;                   // tiles in flight per wavefront
 template <int D>
 constexpr int few_pitch() { return 2 * D + 16; }             // bytes per token: 16 rows' 16-byte reads fall on all banks
 template <int D>
@@ -253,6 +364,75 @@ constexpr int few_patch(int nt) { return 32 * few_pitch<D>() > 16 * nt * D * 4 ?
 template <int D>
 constexpr int few_lds(int nt) { return kFewWaves * (few_patch<D>(nt) + 16 * nt * 8); }
 constexpr int few_waves_per_simd(int D, int NT) { return D * NT <= 128 ? 4 : D * NT <= 256 ? 2 : 1; }
+
+// How a call's work is dealt to workgroups where it is split: in units of 128 tokens (a 32-token tile per wavefront), counted over
+// sequences, their key-value heads and their tiles of rows.  Workgroup g of n takes units [g total / n, (g + 1) total / n), whatever
+// the lengths are: a run of rows' tokens that begins or ends inside one (seq, head, tile).  Those two leave parts in the workspace, at
+// 2 g (begun by another workgroup) and 2 g + 1 (begun here); what lies between them is finished here.  The workgroup that begins
+// rows that others go on with records so, and attn_few_join_kernel adds the parts of its workgroup and of those behind it.
+constexpr int kUnit = 32 * kFewWaves, kLeastUnits = 4;       // at least so many units per workgroup
+struct Load {
+  int first, end, units, tiles;                              // tokens that any row sees, in units; tiles of rows
+  int64_t total;                                             // units x tiles x key-value heads
+  __device__ __forceinline__ Load(const AttnArgs& a, const Sequence& s, int rows) {
+    first = end = 0;
+    if (s.n > 0) {
+      first = s.first(a, 0) & ~31;
+      end = s.last(a, s.n - 1) + 1;
+    }
+    units = end > first ? (end - first + kUnit - 1) / kUnit : 1;   // (rows that see nothing are written too)
+    tiles = (s.n * a.group + rows - 1) / rows;
+    total = (int64_t)units * tiles * a.g.kv_heads;
+  }
+};
+struct Share {
+  int64_t begin, end, total;                                 // this workgroup's units; all
+  int seq, item, off, n;                                     // where `begin` is: sequence, item in it, unit of the item; workgroups that have any
+  __device__ __forceinline__ int workgroup_of(int64_t unit) const { return (int)(((unit + 1) * n - 1) / total); }
+};
+__device__ __forceinline__ void find_share(const AttnArgs& a, int rows, Share& share, int64_t (&wave_sum)[kFewWaves]) {
+  const int each = (a.n_seq + 64 * kFewWaves - 1) / (64 * kFewWaves), lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int s0 = (int)threadIdx.x * each, s1 = s0 + each < a.n_seq ? s0 + each : a.n_seq;
+  int64_t mine = 0;
+  for (int s = s0; s < s1; ++s) mine += Load(a, Sequence(a, s), rows).total;
+  int64_t upto = mine;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int64_t x = __shfl_up(upto, d);
+    upto += lane >= d ? x : 0;
+  }
+  if (lane == 63) wave_sum[wave] = upto;
+  if (threadIdx.x == 0) share.begin = share.end = 0;
+  __syncthreads();
+  int64_t total = 0;
+#pragma unroll
+  for (int w = 0; w < kFewWaves; ++w) {
+    if (w < wave) upto += wave_sum[w];
+    total += wave_sum[w];
+  }
+  const int64_t most = (total + kLeastUnits - 1) / kLeastUnits;
+  const int64_t n = most < (int64_t)gridDim.x ? most : (int64_t)gridDim.x;
+  if ((int64_t)blockIdx.x < n) {
+    const int64_t begin = blockIdx.x * total / n, end = (blockIdx.x + 1) * total / n;
+    int64_t before = upto - mine;
+    if (begin >= before && begin < upto)                     // one lane: the sequence is one of its own
+      for (int s = s0; s < s1; ++s) {
+        const Load load(a, Sequence(a, s), rows);
+        if (begin < before + load.total) {
+          share.begin = begin;
+          share.end = end;
+          share.total = total;
+          share.seq = s;
+          share.item = (int)((begin - before) / load.units);
+          share.off = (int)((begin - before) % load.units);
+          share.n = (int)n;
+          break;
+        }
+        before += load.total;
+      }
+  }
+  __syncthreads();
+}
 
 // NT tiles of 16 rows; TERMS: bf16 terms of P
 template <int D, int MODE, int NT, int TERMS>
@@ -264,14 +444,63 @@ __global__ void __launch_bounds__(64 * kFewWaves, few_waves_per_simd(D, NT)) att
   const int col = lane & 15, quarter = lane >> 4;
   uint8_t* const patch = lds + wave * PATCH;                 // a tile's keys, then its values
   float* const ml = reinterpret_cast<float*>(lds + kFewWaves * PATCH);   // [wave][row][2]
-  const Work w(a);
-  const Sequence s(a, w.seq);
-  const int R = s.n * a.group;
   // this lane's blocks of a tile: its token (16 lanes in a row have 16 tokens: their stores fall on all banks), its block of the token
   const auto token_of = [&](int i) { return D == 256 ? 16 * (i >> 1) + (lane & 15) : LANE_TOKENS * i + (lane & (LANE_TOKENS - 1)); };
   const auto block_of = [&](int i) { return D == 256 ? 4 * (i & 1) + (lane >> 4) : lane / LANE_TOKENS; };
-  for (int r0 = w.tile * 16 * NT; r0 < R; r0 += a.row_tiles * 16 * NT) {
-    const Span span(a, s, r0, R - r0 < 16 * NT ? R - r0 : 16 * NT, w.split);
+  // What to do: rows r0 ... of one key-value head of a sequence, over a span of its tokens
+  constexpr int ROWS = 16 * NT;
+  __shared__ Share share;
+  __shared__ int64_t wave_sum[kFewWaves];
+  int seq, kv_head = 0, tile = 0, item = 0, off = 0;
+  int64_t left = 0;                                          // units; not used where a workgroup has whole items (a.direct)
+  if (a.direct) {
+    const Work w(a);
+    seq = w.seq;
+    kv_head = w.head;
+    tile = w.tile;
+  } else {
+    find_share(a, ROWS, share, wave_sum);
+    if (threadIdx.x == 0) a.joins[4 * blockIdx.x] = -1;
+    left = uniform(share.end) - uniform(share.begin);
+    if (left == 0) return;
+    seq = uniform(share.seq);
+    item = uniform(share.item);
+    off = uniform(share.off);
+  }
+  for (;;) {
+    const Sequence s(a, seq);
+    const int R = s.n * a.group;
+    Span span(0, 0);
+    int part = -1;                                           // where the result goes: out, or among the parts
+    if (a.direct) {
+      if (tile * ROWS >= R) break;
+      span = Span(a, s, tile * ROWS, R - tile * ROWS < ROWS ? R - tile * ROWS : ROWS, 0);
+    } else {
+      const Load load(a, s, ROWS);
+      if (item >= load.tiles * a.g.kv_heads) {               // on to the next sequence
+        ++seq;
+        item = 0;
+        continue;
+      }
+      const int till = left < load.units - off ? off + (int)left : load.units;
+      kv_head = item / load.tiles;
+      tile = item - kv_head * load.tiles;
+      span = Span(load.first + off * kUnit, till == load.units ? load.end : load.first + till * kUnit);
+      if (off > 0 || till < load.units) {
+        part = 2 * (int)blockIdx.x + (off == 0 ? 1 : 0);
+        if (off == 0 && threadIdx.x == 0) {                  // the first part of these rows: the join goes on to the last one's workgroup
+          int32_t* const j = a.joins + 4 * blockIdx.x;
+          j[1] = kv_head;
+          j[2] = tile * ROWS;
+          j[3] = share.workgroup_of(share.end - left + load.units - 1);
+          j[0] = seq;
+        }
+      }
+      left -= till - off;
+      off = 0;
+      ++item;
+    }
+    const int r0 = tile * ROWS;
     // this lane's rows, as operands of the first product: channels 32 st + 8 quarter ... + 7
     Operand q[NT][DB];
     int first[NT], last[NT];
@@ -281,7 +510,7 @@ __global__ void __launch_bounds__(64 * kFewWaves, few_waves_per_simd(D, NT)) att
       const bool there = r < R;
       first[t] = there ? s.first(a, i) : 1;
       last[t] = there ? s.last(a, i) : 0;
-      const uint16_t* p = a.q + (s.q0 + (there ? i : 0)) * a.ld_q + (int64_t)(w.head * a.group + (there ? r - i * a.group : 0)) * D + 8 * quarter;
+      const uint16_t* p = a.q + (s.q0 + (there ? i : 0)) * a.ld_q + (int64_t)(kv_head * a.group + (there ? r - i * a.group : 0)) * D + 8 * quarter;
 #pragma unroll
       for (int st = 0; st < DB; ++st) {
         const u32x4 x = *reinterpret_cast<const u32x4*>(p + 32 * st);
@@ -303,33 +532,36 @@ __global__ void __launch_bounds__(64 * kFewWaves, few_waves_per_simd(D, NT)) att
     // The wavefront's tiles: span.begin + 32 wave, and every 32 kFewWaves tokens from there.  Lane n holds the page of half n % 2 of
     // tile n / 2 of the next 32 tiles (-1: none), so that a tile's addresses wait for no table.
     const int begin = span.begin + 32 * wave;
-    int tile = 0;
+    int fetched = 0;                                         // tiles
     int32_t pages = -1;
-    Block kb[NB], vb[NB];
-    bool held0 = false, held1 = false;                       // whether the tile's two halves have a page
-    const auto fetch = [&](int t) {
-      if ((tile & 31) == 0) pages = page_of(a, s, (int64_t)t + 32 * kFewWaves * (lane >> 1) + 16 * (lane & 1));
-      const Page p0(a, w.head, __builtin_amdgcn_readlane(pages, 2 * (tile & 31)), t), p1(a, w.head, __builtin_amdgcn_readlane(pages, 2 * (tile & 31) + 1), t + 16);
-      held0 = p0.held;
-      held1 = p1.held;
-      ++tile;
+    struct Fetched {                                         // a tile's blocks on their way, and whether its halves have a page
+      Block k[NB], v[NB];
+      bool held0, held1;
+    } ahead[kFewAhead];
+    const auto fetch = [&](Fetched& f, int t) {
+      if (t >= span.end) return;
+      if ((fetched & 31) == 0) pages = page_of(a, s, (int64_t)t + 32 * kFewWaves * (lane >> 1) + 16 * (lane & 1));
+      const Page p0(a, kv_head, __builtin_amdgcn_readlane(pages, 2 * (fetched & 31)), t), p1(a, kv_head, __builtin_amdgcn_readlane(pages, 2 * (fetched & 31) + 1), t + 16);
+      f.held0 = p0.held;
+      f.held1 = p1.held;
+      ++fetched;
 #pragma unroll
       for (int i = 0; i < NB; ++i) {
         const int token = token_of(i);
         const bool second = D == 64 ? token >= 16 : i >= NB / 2;
         const uint8_t* rec = second ? p1.rec : p0.rec;
         const int row = second ? p1.at + (token & 15) : p0.at + token;
-        kb[i] = load_block<D, MODE>(rec, a.g, row, block_of(i));
-        vb[i] = load_block<D, MODE>(rec + a.g.part_bytes, a.g, row, block_of(i));
+        f.k[i] = load_block<D, MODE>(rec, a.g, row, block_of(i));
+        f.v[i] = load_block<D, MODE>(rec + a.g.part_bytes, a.g, row, block_of(i));
       }
     };
-    if (begin < span.end) fetch(begin);
-    for (int t0 = begin; t0 < span.end; t0 += 32 * kFewWaves) {
-      const bool h0 = held0, h1 = held1;
+    const auto take = [&](Fetched& f, int t0) {
+      if (t0 >= span.end) return;
+      const bool h0 = f.held0, h1 = f.held1;
       uint64_t nan[NB];                                      // lanes whose block of V is NaN: zeros here, put in behind the product
       uint64_t any = 0;
 #pragma unroll
-      for (int i = 0; i < NB; ++i) expand<MODE>(kb[i], false, patch + token_of(i) * PITCH + block_of(i) * 64);
+      for (int i = 0; i < NB; ++i) expand<MODE>(f.k[i], false, patch + token_of(i) * PITCH + block_of(i) * 64);
       __builtin_amdgcn_wave_barrier();
       f32x4 sc[NT][2];
 #pragma unroll
@@ -351,12 +583,12 @@ __global__ void __launch_bounds__(64 * kFewWaves, few_waves_per_simd(D, NT)) att
       for (int i = 0; i < NB; ++i) {
         const int token = token_of(i);
         const bool dead = t0 + token >= span.end || !(token >= 16 ? h1 : h0);
-        nan[i] = __ballot(vb[i].scale == 255u && !dead);
+        nan[i] = __ballot(f.v[i].scale == 255u && !dead);
         any |= nan[i];
-        expand<MODE>(vb[i], dead || vb[i].scale == 255u, patch + token * PITCH + block_of(i) * 64);
+        expand<MODE>(f.v[i], dead || f.v[i].scale == 255u, patch + token * PITCH + block_of(i) * 64);
       }
       __builtin_amdgcn_wave_barrier();
-      if (t0 + 32 * kFewWaves < span.end) fetch(t0 + 32 * kFewWaves);
+      fetch(f, t0 + kFewAhead * 32 * kFewWaves);
       const bool whole = h0 && h1 && t0 >= all_from && t0 + 31 <= all_to && t0 + 32 <= span.end;   // (uniform)
       if (!whole) {
 #pragma unroll
@@ -376,10 +608,10 @@ __global__ void __launch_bounds__(64 * kFewWaves, few_waves_per_simd(D, NT)) att
         mx = fmaxf(m[t], max_across_32(max_across_16(mx)));
         const float base = zero_if_none(mx) * a.scale;
         if (__any(mx != m[t])) {
-          const float f = exp2_of(m[t] * a.scale - base);
-          l[t] *= f;
+          const float fade = exp2_of(m[t] * a.scale - base);
+          l[t] *= fade;
 #pragma unroll
-          for (int d = 0; d < D / 16; ++d) o[t][d] *= f;
+          for (int d = 0; d < D / 16; ++d) o[t][d] *= fade;
           m[t] = mx;
         }
         l[t] += weights<TERMS>(sc[t][0], sc[t][1], a.scale, base, p[t]);
@@ -396,21 +628,31 @@ __global__ void __launch_bounds__(64 * kFewWaves, few_waves_per_simd(D, NT)) att
           for (int c = 0; c < TERMS; ++c) o[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v.v, p[t][c].v, o[t][d], 0, 0, 0);
       }
       if (any) {                                             // NaN blocks of V, for the rows that see them
+#pragma unroll 1
+        for (int i = 0; i < NB; ++i) {
+          uint64_t left = nan[0];
 #pragma unroll
-        for (int i = 0; i < NB; ++i)
-          for (uint64_t left = nan[i]; left; left &= left - 1) {
+          for (int k = 1; k < NB; ++k) left = i == k ? nan[k] : left;
+          for (; left; left &= left - 1) {
             const int who = __builtin_ctzll(left), tok = t0 + __builtin_amdgcn_readlane(token_of(i), who), blk = __builtin_amdgcn_readlane(block_of(i), who);
 #pragma unroll
-            for (int t = 0; t < NT; ++t)
-              if (tok >= first[t] && tok <= last[t]) {
+            for (int t = 0; t < NT; ++t) {
+              const bool seen = tok >= first[t] && tok <= last[t];
 #pragma unroll
-                for (int d = 0; d < D / 16; ++d)
-                  if (d / 2 == blk) o[t][d] = f32x4{1, 1, 1, 1} * __uint_as_float(0x7FC00000u);
-              }
+              for (int d = 0; d < D / 16; ++d)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) o[t][d][j] = seen && d / 2 == blk ? __uint_as_float(0x7FC00000u) : o[t][d][j];
+            }
           }
+        }
       }
       __builtin_amdgcn_wave_barrier();
-    }
+    };
+#pragma unroll
+    for (int u = 0; u < kFewAhead; ++u) fetch(ahead[u], begin + u * 32 * kFewWaves);
+    for (int t0 = begin; t0 < span.end; t0 += kFewAhead * 32 * kFewWaves)
+#pragma unroll
+      for (int u = 0; u < kFewAhead; ++u) take(ahead[u], t0 + u * 32 * kFewWaves);
     // join the wavefronts: each leaves its rows in its own patch
     float* const mine = reinterpret_cast<float*>(patch);
 #pragma unroll
@@ -438,11 +680,44 @@ __global__ void __launch_bounds__(64 * kFewWaves, few_waves_per_simd(D, NT)) att
         sum += ml[(v * 16 * NT + row) * 2 + 1] * f;
         out += *reinterpret_cast<const f32x4*>(lds + v * PATCH + (row * D + d) * 4) * f;
       }
-      const int i = r / a.group, head = w.head * a.group + r - i * a.group;
-      finish_values(a, w.split, s.q0 + i, head, d, out, sum);
-      if (d == 0) finish_row(a, w.split, s.q0 + i, head, top, sum);
+      const int i = r / a.group, head = kv_head * a.group + r - i * a.group;
+      if (part < 0) {
+        store_out(a, s.q0 + i, head, d, sum == 0.0f ? f32x4{0, 0, 0, 0} : out / sum);
+        if (d == 0 && a.lse) a.lse[(s.q0 + i) * a.heads + head] = lse_of(top, sum);
+      } else {
+        const int64_t at = (int64_t)part * 16 * NT + row;
+        *reinterpret_cast<f32x4*>(a.part_o + at * D + d) = out;
+        if (d == 0) {
+          a.part_ml[2 * at] = top;
+          a.part_ml[2 * at + 1] = sum;
+        }
+      }
     }
     __syncthreads();
+    if (a.direct) tile += a.row_tiles;
+    else if (left == 0) break;
+  }
+}
+
+// The joins that Share records, `each` workgroups' records per workgroup here: a row at a time by a wavefront, or by the workgroup
+// where the parts are many.
+__global__ void __launch_bounds__(256) attn_few_join_kernel(const AttnArgs a, int rows_per_tile, int n_records, int each) {
+  __shared__ JoinRoom room;
+  const int lane = threadIdx.x & 63, first = (int)blockIdx.x * each;
+  uint64_t todo = __ballot(lane < each && first + lane < n_records && a.joins[4 * (first + lane)] >= 0);
+  for (; todo; todo &= todo - 1) {                           // (the same in every wavefront)
+    const int g = first + __builtin_ctzll(todo);
+    const int32_t* const j = a.joins + 4 * g;
+    const Sequence s(a, j[0]);
+    const int kv_head = j[1], r0 = j[2], parts = j[3] - g + 1, R = s.n * a.group;
+    const bool by_wave = parts <= 64;
+    const int step = (by_wave ? 4 : 1) * (int)gridDim.y;
+    for (int row = by_wave ? (int)blockIdx.y * 4 + (int)(threadIdx.x >> 6) : (int)blockIdx.y; row < rows_per_tile && r0 + row < R; row += step) {
+      const int r = r0 + row, i = r / a.group;
+      const auto part_at = [&](int p) { return ((int64_t)2 * (g + p) + (p == 0 ? 1 : 0)) * rows_per_tile + row; };
+      if (by_wave) join_row_by_wave(a, parts, part_at, s.q0 + i, kv_head * a.group + r - i * a.group);
+      else join_row(a, room, parts, part_at, s.q0 + i, kv_head * a.group + r - i * a.group);
+    }
   }
 }
 
@@ -498,21 +773,21 @@ __global__ void __launch_bounds__(64 * kManyWaves) attn_many_kernel(const AttnAr
       for (int j = 0; j < 16; ++j) o[d][j] = 0.0f;
     Block kb[NL], vb[NL];
     uint32_t held = 0, held_next = 0;                        // bit j: tokens 16 j ... + 15 of the tile have a page
-    int tile = 0;
+    int fetched = 0;                                         // tiles
     int32_t pages = -1;                                      // lane n: the page of tokens 16 (n % 4) ... of tile n / 4 of the next 16
     const auto fetch = [&](int t) {
-      if ((tile & 15) == 0) pages = page_of(a, s, (int64_t)t + 16 * lane);
+      if ((fetched & 15) == 0) pages = page_of(a, s, (int64_t)t + 16 * lane);
       held_next = 0;
       const uint8_t* rec[4];
       int at[4];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const Page p(a, w.head, __builtin_amdgcn_readlane(pages, 4 * (tile & 15) + j), t + 16 * j);
+        const Page p(a, w.head, __builtin_amdgcn_readlane(pages, 4 * (fetched & 15) + j), t + 16 * j);
         held_next |= (p.held ? 1u : 0u) << j;
         rec[j] = p.rec;
         at[j] = p.at;
       }
-      ++tile;
+      ++fetched;
 #pragma unroll
       for (int k = 0; k < NL; ++k) {
         const int n = (int)threadIdx.x + 64 * kManyWaves * k, token = n / DB;
@@ -644,65 +919,29 @@ __global__ void __launch_bounds__(64 * kManyWaves) attn_many_kernel(const AttnAr
   }
 }
 
-// ---- the parts of split sequences ---------------------------------------------------------------------------------------
-// A workgroup per (row, head): every lane the weight of one part (at most kMostSplits = lanes), then D / 4 lanes across a row and
-// 1024 / D parts at a time.  Rows that no sequence has are left as they are.
-constexpr int kMostSplits = 256;
-__global__ void __launch_bounds__(256) attn_join_kernel(const AttnArgs a) {
-  __shared__ float weight[kMostSplits], top_of[4], sum_of[4];
-  __shared__ __attribute__((aligned(16))) float acc[1024];
-  const int t = threadIdx.x, across = a.g.D >> 2, d = 4 * (t & (across - 1)), g = t / across, groups = 256 / across;
+// ---- the parts of split sequences: many rows ---------------------------------------------------------------------------
+// Parts [split][row][head].  Rows that no sequence has are left as they are.
+__global__ void __launch_bounds__(256) attn_many_join_kernel(const AttnArgs a) {
+  __shared__ JoinRoom room;
   const int64_t from = a.q_start ? a.q_start[0] : 0, to = a.q_start ? a.q_start[a.n_seq] : a.rows, n = a.rows * a.heads;
   for (int64_t j = blockIdx.x; j < n; j += gridDim.x) {
     const int64_t row = j / a.heads;
-    if (row < from || row >= to) continue;                   // (the whole workgroup)
-    const int head = (int)(j - row * a.heads);
-    float m = -kInf, l = 0.0f;
-    if (t < a.splits) {
-      m = a.part_ml[(t * n + j) * 2];
-      l = a.part_ml[(t * n + j) * 2 + 1];
-    }
-    float top = m;
-#pragma unroll
-    for (int x = 32; x >= 1; x >>= 1) top = fmaxf(top, __shfl_xor(top, x));
-    if ((t & 63) == 0) top_of[t >> 6] = top;
-    __syncthreads();
-    top = fmaxf(fmaxf(top_of[0], top_of[1]), fmaxf(top_of[2], top_of[3]));
-    const float f = l == 0.0f ? 0.0f : exp2_of(m - zero_if_none(top));   // (0: a part that saw nothing, left out below)
-    weight[t] = f;
-    float sum = l * f;
-#pragma unroll
-    for (int x = 32; x >= 1; x >>= 1) sum += __shfl_xor(sum, x);
-    if ((t & 63) == 0) sum_of[t >> 6] = sum;
-    __syncthreads();
-    sum = (sum_of[0] + sum_of[1]) + (sum_of[2] + sum_of[3]);
-    f32x4 out = {0, 0, 0, 0};
-#pragma unroll 4
-    for (int p = g; p < a.splits; p += groups) {
-      const float w = weight[p];
-      const f32x4 x = *reinterpret_cast<const f32x4*>(a.part_o + (p * n + j) * a.g.D + d);
-      if (w != 0.0f) out += x * w;
-    }
-    *reinterpret_cast<f32x4*>(acc + 4 * t) = out;
-    __syncthreads();
-    if (g == 0) {
-      for (int p = 1; p < groups; ++p) out += *reinterpret_cast<const f32x4*>(acc + 4 * (t + p * across));
-      store_out(a, row, head, d, sum == 0.0f ? f32x4{0, 0, 0, 0} : out / sum);
-    }
-    if (t == 0 && a.lse) a.lse[row * a.heads + head] = lse_of(top, sum);
-    __syncthreads();
+    if (row >= from && row < to) join_row(a, room, a.splits, [&](int p) { return p * n + j; }, row, (int)(j - row * a.heads));
   }
 }
 
 // ---- launch -----------------------------------------------------------------------------------------------------------
 struct Plan {
-  bool many;
+  bool many, direct;
   int nt, row_tiles, splits, chunk;
   int64_t wgs;
 };
 
-// Which kernel, and over how many workgroups a sequence's tokens are split.  Up to 32 rows of a key-value head: attn_few_kernel.
-Plan plan_for(int64_t n_seq, int64_t max_q, int64_t max_kv, int64_t heads, int64_t kv_heads, int64_t window) {
+// Sequences of at most so many tokens are not dealt out in parts: a workgroup goes over them in less than the parts' join takes.
+constexpr int64_t kDirectTokens = 2048;
+
+// Which kernel, and how a sequence's tokens are dealt to workgroups.  Up to 32 rows of a key-value head: attn_few_kernel.
+Plan plan_for(int64_t n_seq, int64_t max_q, int64_t max_kv, int64_t heads, int64_t kv_heads, int64_t D, int64_t window) {
   Plan p;
   const int64_t rows = max_q * (heads / kv_heads);           // of one key-value head
   p.many = rows > 32;
@@ -710,26 +949,37 @@ Plan plan_for(int64_t n_seq, int64_t max_q, int64_t max_kv, int64_t heads, int64
   const int64_t tile = p.many ? kManyRows : 16 * p.nt;
   p.row_tiles = (int)((rows + tile - 1) / tile);
   if (p.row_tiles < 1) p.row_tiles = 1;
-  const int64_t base = n_seq * kv_heads * p.row_tiles;
-  // tokens that one tile of rows goes over, at most
-  int64_t len = max_kv;
+  const int64_t items = n_seq * kv_heads * p.row_tiles;
+  int64_t len = max_kv;                                      // tokens that one tile of rows goes over, at most
   if (window > 0 && window + max_q + 32 < len) len = window + max_q + 32;
-  const int64_t least = p.many ? 512 : 256, want = 1024;     // tokens per workgroup at least; workgroups wanted
-  int64_t splits = base < want ? (want + base - 1) / base : 1;
+  p.direct = false;
+  p.splits = 1;
+  p.chunk = 1 << 30;
+  p.wgs = items;
+  if (!p.many) {
+    const int64_t room = (int64_t)kNumCU * few_waves_per_simd((int)D, p.nt), units = items * ((len + kUnit - 1) / kUnit);
+    p.direct = len <= kDirectTokens || items >= 4 * room;
+    if (!p.direct) p.wgs = units < kLeastUnits * room ? (units + kLeastUnits - 1) / kLeastUnits : room;
+    return p;
+  }
+  const int64_t least = 512, want = 1024;                    // tokens per workgroup at least; workgroups wanted
+  int64_t splits = items < want ? (want + items - 1) / items : 1;
   if (splits > (len + least - 1) / least) splits = (len + least - 1) / least;
   if (splits < 1) splits = 1;
-  if (splits > kMostSplits) splits = kMostSplits;
-  const int64_t step = p.many ? kManyTokens : 32 * kFewWaves;
-  const int64_t chunk = ((len + splits - 1) / splits + step - 1) / step * step;
-  p.chunk = (int)(chunk < step ? step : chunk > (1 << 30) ? (1 << 30) : chunk);
+  const int64_t chunk = ((len + splits - 1) / splits + kManyTokens - 1) / kManyTokens * kManyTokens;
+  p.chunk = (int)(chunk < kManyTokens ? kManyTokens : chunk > (1 << 30) ? (1 << 30) : chunk);
   p.splits = (int)((len + p.chunk - 1) / p.chunk);
   if (p.splits < 1) p.splits = 1;
-  p.wgs = base * p.splits;
+  p.wgs = items * p.splits;
   return p;
 }
 
+// Workspace: values of the parts, their maxima and sums, records of joins
+int64_t part_rows(const Plan& p, int64_t rows, int64_t heads) {
+  return p.many ? (p.splits > 1 ? p.splits * rows * heads : 0) : p.direct ? 0 : p.wgs * 2 * 16 * p.nt;
+}
 size_t parts_bytes(const Plan& p, int64_t rows, int64_t heads, int64_t D) {
-  return p.splits > 1 ? (size_t)p.splits * (size_t)rows * (size_t)heads * (size_t)(D + 2) * 4 : 0;
+  return (size_t)part_rows(p, rows, heads) * (size_t)(D + 2) * 4 + (p.many || p.direct ? 0 : (size_t)p.wgs * 16);
 }
 
 template <int D, int MODE, int TERMS>
@@ -758,7 +1008,7 @@ bool shapes_fit(int64_t n_seq, int64_t rows, int64_t max_q, int64_t max_kv, int6
 extern "C" size_t mxp_attention_workspace_bytes(int64_t n_seq, int64_t rows, int64_t max_q, int64_t max_kv, int64_t heads, int64_t kv_heads,
                                                 int64_t head_dim, int64_t window) {
   if (!shapes_fit(n_seq, rows, max_q, max_kv, heads, kv_heads) || n_seq == 0 || rows == 0 || rows * heads > kMostRows || head_dim < 1 || window < 0) return 0;
-  return parts_bytes(plan_for(n_seq, max_q < rows ? max_q : rows, max_kv, heads, kv_heads, window), rows, heads, head_dim);
+  return parts_bytes(plan_for(n_seq, max_q < rows ? max_q : rows, max_kv, heads, kv_heads, head_dim, window), rows, heads, head_dim);
 }
 
 extern "C" int mxp_attention(const void* Q, int q_dtype, int64_t ld_q, int64_t rows, int64_t heads, const int32_t* q_start, const int32_t* kv_len,
@@ -782,7 +1032,7 @@ extern "C" int mxp_attention(const void* Q, int q_dtype, int64_t ld_q, int64_t r
   if (!aligned16(Q) || !aligned16(O) || !aligned16(cache) || !aligned16(workspace) || ld_q * 2 % 16 != 0 || ld_o * osz % 16 != 0 || off4(q_start) ||
       off4(kv_len) || off4(table) || off4(lse))
     return MXP_ERR_ALIGN;
-  const Plan p = plan_for(n_seq, max_q < rows ? max_q : rows, max_kv, heads, kv_heads, window);
+  const Plan p = plan_for(n_seq, max_q < rows ? max_q : rows, max_kv, heads, kv_heads, head_dim, window);
   if (p.wgs > 2147483647LL) return MXP_ERR_UNSUPPORTED;
   const size_t need = parts_bytes(p, rows, heads, head_dim);
   if (need > 0 && (!workspace || workspace_bytes < need)) return MXP_ERR_WORKSPACE;
@@ -807,7 +1057,10 @@ extern "C" int mxp_attention(const void* Q, int q_dtype, int64_t ld_q, int64_t r
   a.o_bf16 = o_dtype == MXP_BF16;
   a.lse = lse;
   a.part_o = static_cast<float*>(workspace);
-  a.part_ml = need ? a.part_o + (size_t)p.splits * rows * heads * head_dim : nullptr;
+  const size_t parts = (size_t)part_rows(p, rows, heads);
+  a.part_ml = need ? a.part_o + parts * head_dim : nullptr;
+  a.joins = need ? reinterpret_cast<int32_t*>(a.part_ml + 2 * parts) : nullptr;
+  a.direct = p.direct ? 1 : 0;
   a.splits = p.splits;
   a.chunk = p.chunk;
   a.row_tiles = p.row_tiles;
@@ -819,9 +1072,18 @@ extern "C" int mxp_attention(const void* Q, int q_dtype, int64_t ld_q, int64_t r
   else MXP_ATTN_M(256);
 #undef MXP_ATTN_M
 #undef MXP_ATTN_T
-  if (p.splits > 1) {
+  if (p.many && p.splits > 1) {
     const int64_t want = rows * heads;
-    hipLaunchKernelGGL(attn_join_kernel, dim3((unsigned)(want < (1 << 20) ? want : (1 << 20))), dim3(256), 0, s, a);
+    hipLaunchKernelGGL(attn_many_join_kernel, dim3((unsigned)(want < (1 << 20) ? want : (1 << 20))), dim3(256), 0, s, a);
+  } else if (!p.many && !p.direct) {
+    // Where many parts are to be joined there are few records: 16 of them and one row per workgroup (one sequence of 131000 tokens,
+    // 8 joins of 128 parts: 14.6 -> 7.8 us against a record each); else a record per workgroup and a row per wavefront.
+    int64_t most = (max_q < rows ? max_q : rows) * a.group;
+    most = most < 1 ? 1 : most < 16 * p.nt ? most : 16 * p.nt;
+    const bool many_parts = p.wgs > 32 * n_seq * kv_heads * p.row_tiles;
+    const int each = many_parts ? 16 : 1;
+    hipLaunchKernelGGL(attn_few_join_kernel, dim3((unsigned)((p.wgs + each - 1) / each), (unsigned)(many_parts ? most : (most + 3) / 4)), dim3(256), 0, s, a, 16 * p.nt,
+                       (int)p.wgs, each);
   }
   return launch_status();
 }
