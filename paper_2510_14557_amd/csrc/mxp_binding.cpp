@@ -25,6 +25,12 @@ struct Entry {
   decltype(&mxp_gemm_decode_bf16a) decode_bf16a;
   decltype(&mxp_gemm_w4a16_ws) w4a16;
   decltype(&mxp_gemm_w4a16_workspace_bytes) w4a16_ws;
+  decltype(&mxp_rmsnorm_quantize) rmsnorm_quantize;
+  decltype(&mxp_cache_bytes) cache_bytes;
+  decltype(&mxp_cache_write) cache_write;
+  decltype(&mxp_cache_read) cache_read;
+  decltype(&mxp_attention) attention;
+  decltype(&mxp_attention_workspace_bytes) attention_ws;
 } lib = {};
 
 // a plain CUDA tensor, or nullptr
@@ -212,9 +218,151 @@ PyObject* fast_gemm_w4a16(PyObject*, PyObject* const* a, Py_ssize_t n) {   // ac
   END_HANDLE_TH_ERRORS
 }
 
+// ---- norm, cache, attention: besides, every tensor lies on the current device and has the shape that the others say -----
+bool here(const at::Tensor* t) { return t && t->device().index() == c10::hip::getCurrentHIPStream().device_index(); }
+bool none_or_tensor(PyObject* o, const at::Tensor*& t) {
+  t = o == Py_None ? nullptr : tensor(o);
+  return o == Py_None || here(t);
+}
+void* data(const at::Tensor* t) { return t ? t->data_ptr() : nullptr; }
+bool real(PyObject* o, float& v) {
+  if (!PyFloat_CheckExact(o)) return false;
+  v = (float)PyFloat_AS_DOUBLE(o);
+  return true;
+}
+bool whole(const at::Tensor* t, at::ScalarType type, int64_t dims) { return here(t) && t->scalar_type() == type && t->dim() == dims && t->is_contiguous(); }
+int dtype_code(const at::Tensor& t) { return t.scalar_type() == at::kFloat ? MXP_F32 : t.scalar_type() == at::kBFloat16 ? MXP_BF16 : -1; }
+// [rows][heads][D] without gaps inside a row
+bool heads_of(const at::Tensor* t, int64_t rows, int64_t heads, int64_t D) {
+  return here(t) && t->dim() == 3 && (rows < 0 || t->size(0) == rows) && (heads < 0 || t->size(1) == heads) && t->size(2) == D && t->stride(2) == 1 &&
+         (t->size(1) == 1 || t->stride(1) == D) && dtype_code(*t) >= 0;
+}
+int64_t ld3(const at::Tensor& t) { return t.size(0) > 1 ? t.stride(0) : std::max<int64_t>(t.size(1) * t.size(2), 1); }
+
+struct Cache {                                               // data, and page_tokens, kv_heads, head_dim, fmt
+  const at::Tensor* t = nullptr;
+  int64_t pages = 0, page = 0, heads = 0, D = 0, fmt = 0;
+  bool take(PyObject* d, PyObject* const* geometry) {
+    t = tensor(d);
+    if (!whole(t, at::kByte, 4)) return false;
+    pages = t->size(0);
+    page = integer(geometry[0]);
+    heads = integer(geometry[1]);
+    D = integer(geometry[2]);
+    fmt = integer(geometry[3]);
+    return fmt >= 0 && fmt <= MXP_FMT_MXFP8P && t->numel() > 0 && t->size(1) == heads && (size_t)t->numel() == lib.cache_bytes(pages, page, heads, D, (int)fmt);
+  }
+};
+
+PyObject* fast_rmsnorm_quantize(PyObject*, PyObject* const* a, Py_ssize_t n) {   // x, weight, residual or None, eps, fmt
+  HANDLE_TH_ERRORS
+  if (!arguments(a, n, 5, 4)) Py_RETURN_NONE;
+  const at::Tensor *x = tensor(a[0]), *w = tensor(a[1]), *r = nullptr;
+  const int dt = rows_dtype(x);
+  float eps = 0;
+  if (dt < 0 || !here(x) || !here(w) || !none_or_tensor(a[2], r) || !real(a[3], eps)) Py_RETURN_NONE;
+  const int64_t rows = x->size(0), K = x->size(1), fmt = integer(a[4]);
+  if (K % 32 != 0 || fmt < MXP_FMT_MXFP4 || fmt > MXP_FMT_MXFP8P || w->dim() != 1 || w->size(0) != K || w->stride(0) != 1 || dtype_code(*w) < 0) Py_RETURN_NONE;
+  if (r && (rows_dtype(r) != dt || r->size(0) != rows || r->size(1) != K)) Py_RETURN_NONE;
+  at::Tensor e = bytes(*x, {rows, K * code_bits(fmt) / 8}), s = bytes(*x, {rows, K / 32}), i = bytes(*x, {rows, K / 32}), h;
+  if (r) h = output(*x, rows, K, dt);
+  if (unlocked([&] {
+        return lib.rmsnorm_quantize(x->data_ptr(), data(r), dt, rows, K, ld(*x), r ? ld(*r) : 0, w->data_ptr(), dtype_code(*w), eps,
+                                    r ? h.data_ptr() : nullptr, r ? std::max<int64_t>(K, 1) : 0, (int)fmt, static_cast<uint8_t*>(e.data_ptr()),
+                                    static_cast<uint8_t*>(s.data_ptr()), static_cast<uint8_t*>(i.data_ptr()), stream());
+      }) != MXP_OK)
+    Py_RETURN_NONE;
+  PyObject *q = PyTuple_New(3), *out = PyTuple_New(2);
+  if (!q || !out) {
+    Py_XDECREF(q);
+    Py_XDECREF(out);
+    return nullptr;
+  }
+  PyTuple_SET_ITEM(q, 0, THPVariable_Wrap(std::move(e)));
+  PyTuple_SET_ITEM(q, 1, THPVariable_Wrap(std::move(s)));
+  PyTuple_SET_ITEM(q, 2, THPVariable_Wrap(std::move(i)));
+  PyTuple_SET_ITEM(out, 0, q);
+  if (!r) Py_INCREF(a[0]);
+  PyTuple_SET_ITEM(out, 1, r ? THPVariable_Wrap(std::move(h)) : a[0]);
+  return out;
+  END_HANDLE_TH_ERRORS
+}
+
+PyObject* fast_cache_write(PyObject*, PyObject* const* a, Py_ssize_t n) {   // data, k, v, slots, page_tokens, kv_heads, head_dim, fmt
+  HANDLE_TH_ERRORS
+  Cache c;
+  if (!arguments(a, n, 8, 4) || !c.take(a[0], a + 4)) Py_RETURN_NONE;
+  const at::Tensor *k = tensor(a[1]), *v = tensor(a[2]), *slots = tensor(a[3]);
+  if (!whole(slots, at::kLong, 1)) Py_RETURN_NONE;
+  const int64_t tokens = slots->size(0);
+  if (!heads_of(k, tokens, c.heads, c.D) || !heads_of(v, tokens, c.heads, c.D) || k->scalar_type() != v->scalar_type()) Py_RETURN_NONE;
+  if (unlocked([&] {
+        return lib.cache_write(k->data_ptr(), v->data_ptr(), dtype_code(*k), tokens, ld3(*k), ld3(*v), static_cast<const int64_t*>(slots->data_ptr()),
+                               c.t->data_ptr(), c.pages, c.page, c.heads, c.D, (int)c.fmt, stream());
+      }) != MXP_OK)
+    Py_RETURN_NONE;
+  Py_RETURN_TRUE;
+  END_HANDLE_TH_ERRORS
+}
+
+PyObject* fast_cache_read(PyObject*, PyObject* const* a, Py_ssize_t n) {   // data, slots, page_tokens, kv_heads, head_dim, fmt, dtype code
+  HANDLE_TH_ERRORS
+  Cache c;
+  if (!arguments(a, n, 7, 2) || !c.take(a[0], a + 2)) Py_RETURN_NONE;
+  const at::Tensor* slots = tensor(a[1]);
+  const int64_t d = integer(a[6]);
+  if (!whole(slots, at::kLong, 1) || (d != MXP_F32 && d != MXP_BF16)) Py_RETURN_NONE;
+  const int64_t tokens = slots->size(0);
+  const auto opts = at::TensorOptions().dtype(d == MXP_BF16 ? at::kBFloat16 : at::kFloat).device(slots->device());
+  at::Tensor k = at::empty({tokens, c.heads, c.D}, opts), v = at::empty({tokens, c.heads, c.D}, opts);
+  if (unlocked([&] {
+        return lib.cache_read(c.t->data_ptr(), c.pages, c.page, c.heads, c.D, (int)c.fmt, static_cast<const int64_t*>(slots->data_ptr()), tokens,
+                              k.data_ptr(), v.data_ptr(), (int)d, c.heads * c.D, c.heads * c.D, stream());
+      }) != MXP_OK)
+    Py_RETURN_NONE;
+  PyObject* out = PyTuple_New(2);
+  if (!out) return nullptr;
+  PyTuple_SET_ITEM(out, 0, THPVariable_Wrap(std::move(k)));
+  PyTuple_SET_ITEM(out, 1, THPVariable_Wrap(std::move(v)));
+  return out;
+  END_HANDLE_TH_ERRORS
+}
+
+// q, data, table, kv_len, q_start or None, lse or None, scale, causal, window, max_q, max_kv (-1: left out), dtype code, page_tokens, kv_heads, head_dim, fmt
+PyObject* fast_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  Cache c;
+  float scale = 0;
+  const at::Tensor *start = nullptr, *lse = nullptr;
+  if (!arguments(a, n, 16, 7) || !c.take(a[1], a + 12) || !none_or_tensor(a[4], start) || !none_or_tensor(a[5], lse) || !real(a[6], scale)) Py_RETURN_NONE;
+  const at::Tensor *q = tensor(a[0]), *table = tensor(a[2]), *len = tensor(a[3]);
+  const int64_t causal = integer(a[7]), window = integer(a[8]), d = integer(a[11]);
+  int64_t max_q = integer(a[9]), max_kv = integer(a[10]);
+  if (!heads_of(q, -1, -1, c.D) || !whole(len, at::kInt, 1) || !whole(table, at::kInt, 2) || (d != MXP_F32 && d != MXP_BF16)) Py_RETURN_NONE;
+  const int64_t rows = q->size(0), heads = q->size(1), seqs = len->size(0);
+  if (table->size(0) != seqs || (start && (!whole(start, at::kInt, 1) || start->size(0) != seqs + 1)) ||
+      (lse && (!whole(lse, at::kFloat, 2) || lse->size(0) != rows || lse->size(1) != heads)))
+    Py_RETURN_NONE;
+  if (max_q < 0) max_q = start ? rows : 1;
+  if (max_kv < 0) max_kv = std::min<int64_t>(table->size(1) * c.page, (int64_t)1 << 30);
+  at::Tensor out = at::empty({rows, heads, c.D}, at::TensorOptions().dtype(d == MXP_BF16 ? at::kBFloat16 : at::kFloat).device(q->device())), ws;
+  const int64_t need = (int64_t)lib.attention_ws(seqs, rows, max_q, max_kv, heads, c.heads, c.D, window);
+  if (need > 0) ws = bytes(*q, {need});
+  if (unlocked([&] {
+        return lib.attention(q->data_ptr(), dtype_code(*q), ld3(*q), rows, heads, static_cast<const int32_t*>(data(start)), static_cast<const int32_t*>(len->data_ptr()),
+                             static_cast<const int32_t*>(table->data_ptr()), table->size(1), seqs, max_q, max_kv, scale, (int)causal, window, c.t->data_ptr(),
+                             c.pages, c.page, c.heads, c.D, (int)c.fmt, out.data_ptr(), (int)d, heads * c.D, static_cast<float*>(data(lse)),
+                             need > 0 ? ws.data_ptr() : nullptr, (size_t)std::max<int64_t>(need, 0), stream());
+      }) != MXP_OK)
+    Py_RETURN_NONE;
+  return THPVariable_Wrap(std::move(out));
+  END_HANDLE_TH_ERRORS
+}
+
 #define MXP_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(fast_##name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {MXP_METHOD(init),      MXP_METHOD(quantize),          MXP_METHOD(dequantize), MXP_METHOD(gemm),
-                         MXP_METHOD(gemm_bf16a), MXP_METHOD(gemm_decode_bf16a), MXP_METHOD(gemm_w4a16), {nullptr, nullptr, 0, nullptr}};
+                         MXP_METHOD(gemm_bf16a), MXP_METHOD(gemm_decode_bf16a), MXP_METHOD(gemm_w4a16),
+                         MXP_METHOD(rmsnorm_quantize), MXP_METHOD(cache_write), MXP_METHOD(cache_read), MXP_METHOD(attention), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_mxp_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -32,7 +32,8 @@ EXPORTS = ("mxp_quantize", "mxp_quantize_t", "mxp_quantize_gather", "mxp_dequant
 _lib = None
 _fast = None                                               # _mxp_binding or _NoNative, loaded with the library
 _FAST_ENTRIES = ("mxp_quantize", "mxp_dequantize", "mxp_gemm", "mxp_gemm_workspace_bytes_fmt", "mxp_gemm_bf16a", "mxp_gemm_bf16a_workspace_bytes",
-                 "mxp_gemm_decode_bf16a", "mxp_gemm_w4a16_ws", "mxp_gemm_w4a16_workspace_bytes")
+                 "mxp_gemm_decode_bf16a", "mxp_gemm_w4a16_ws", "mxp_gemm_w4a16_workspace_bytes", "mxp_rmsnorm_quantize", "mxp_cache_bytes",
+                 "mxp_cache_write", "mxp_cache_read", "mxp_attention", "mxp_attention_workspace_bytes")
 
 
 class MxpError(RuntimeError):
@@ -620,6 +621,10 @@ def rmsnorm_quantize(x: torch.Tensor, weight: torch.Tensor, fmt: int = MXFP8, re
     """h = x + residual; the root-mean-square norm of h, times weight, quantized -> ((elems, scales, bm_idx), h).
 
     Without a residual h is x itself, and nothing is written unless h is given; h may be x or residual (in place)."""
+    if h is None:
+        q = _native().rmsnorm_quantize(x, weight, residual, eps, fmt)
+        if q is not None:
+            return q
     _here(x, weight, residual, h)
     _dev2d(x)
     rows, K = x.shape
@@ -678,6 +683,8 @@ def _slots(slots: torch.Tensor) -> int:
 def cache_write(cache: KVCache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor):
     """k, v [tokens, kv_heads, head_dim] fp32/bf16 quantized into the slots (int64, page * page_tokens + place; distinct, but for
     those outside the cache, -1 say, whose tokens are not kept) of their tokens."""
+    if _native().cache_write(cache.data, k, v, slots, *cache[1:]):
+        return
     _here(cache.data, k, v, slots)
     n_pages, n = _cache_pages(cache), _slots(slots)
     _like(k, (n, cache.kv_heads, cache.head_dim), v.dtype, "k and v")
@@ -688,6 +695,10 @@ def cache_write(cache: KVCache, k: torch.Tensor, v: torch.Tensor, slots: torch.T
 
 def cache_read(cache: KVCache, slots: torch.Tensor, dtype: torch.dtype = torch.bfloat16, out=None):
     """(k, v) [tokens, kv_heads, head_dim] of the given slots, de-converted; zeros for slots outside the cache."""
+    if out is None:
+        kv = _native().cache_read(cache.data, slots, *cache[1:], _DTYPE_CODE.get(dtype))
+        if kv is not None:
+            return kv
     _here(cache.data, slots, *(out or ()))
     n_pages, n = _cache_pages(cache), _slots(slots)
     shape = (n, cache.kv_heads, cache.head_dim)
@@ -713,6 +724,12 @@ def attention(q: torch.Tensor, cache: KVCache, table: torch.Tensor, kv_len: torc
     of q (None: one each).  scale: head_dim ** -0.5 if left out.  max_q, max_kv: upper bounds on a sequence's queries and tokens, for
     the choice of launch (left out: rows, and what the table has room for).  lse fp32 [rows, heads]: takes log-sum-exp of the scores.
     Rows that belong to no sequence are not written in out and lse."""
+    scale = cache.head_dim ** -0.5 if scale is None else float(scale)
+    if out is None and workspace is None and min(max_q or 0, max_kv or 0) >= 0:
+        out = _native().attention(q, cache.data, table, kv_len, q_start, lse, scale, int(causal), window, -1 if max_q is None else max_q,
+                                  -1 if max_kv is None else max_kv, _DTYPE_CODE.get(out_dtype), *cache[1:])
+        if out is not None:
+            return out
     _here(q, cache.data, table, kv_len, q_start, out, lse, workspace)
     n_pages = _cache_pages(cache)
     if q.dim() != 3 or q.shape[2] != cache.head_dim:
@@ -741,6 +758,6 @@ def attention(q: torch.Tensor, cache: KVCache, table: torch.Tensor, kv_len: torc
     elif workspace.dtype != torch.uint8 or not workspace.is_contiguous():
         raise MxpError("workspace must be a contiguous uint8 tensor")
     _check(lib().mxp_attention(_p(q), _dt(q), _ld(q, "q"), rows, heads, _p(q_start), _p(kv_len), _p(table), table.shape[1], n_seq, max_q, max_kv,
-                               D ** -0.5 if scale is None else scale, int(causal), window, _p(cache.data), n_pages, *cache[1:], _p(out), _dt(out),
+                               scale, int(causal), window, _p(cache.data), n_pages, *cache[1:], _p(out), _dt(out),
                                _ld(out, "out"), _p(lse), _p(workspace), 0 if workspace is None else workspace.numel(), _stream()), "mxp_attention")
     return out

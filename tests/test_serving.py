@@ -510,6 +510,45 @@ def test_binding_refuses_shapes_and_types():
             pytest.fail("call %d was taken" % n)
 
 
+@gpu
+def test_native_calls_are_taken_and_equal_the_general_code(monkeypatch):
+    """The binding's native part takes the ordinary calls of each operator, and gives what the general code gives."""
+    b = Batch("MXFP4PP", 16, 2, 4, 128, [4000, 33, 100], [1, 1, 1], seed=13)
+    r = Batch("MXFP4P", 32, 2, 2, 64, [50, 120], [4, 30], seed=14)
+    cb, cr = b.cache(), r.cache()
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    x, res = (torch.randn((5, 96), generator=gen, device="cuda").bfloat16() for _ in range(2))
+    w = torch.randn(96, generator=gen, device="cuda")
+    k, v = (torch.randn((7, 4, 128), generator=gen, device="cuda")[:, :2] for _ in range(2))
+    slots = torch.tensor([3, -1, 40, 7, 100, 9, 31], device="cuda")
+
+    def calls():
+        mxp.cache_write(cb, k, v, slots)
+        q, h = mxp.rmsnorm_quantize(x, w, mxp.MXFP6P, residual=res)
+        q2, x2 = mxp.rmsnorm_quantize(x, w, mxp.MXFP4PP, eps=0.5)
+        return [*q, h, *q2, x2, cb.data.clone(), *mxp.cache_read(cb, slots), *mxp.cache_read(cb, slots, torch.float32), *b.call(cb), *b.call(cb, max_kv=None, max_q=None),
+                *r.call(cr, out_dtype=torch.float32, window=9), *r.call(cr, causal=False, scale=1)]
+
+    taken = []
+    native = mxp._native()
+
+    class Noting:
+        def __getattr__(self, name):
+            def call(*args):
+                out = getattr(native, name)(*args)
+                taken.append((name, out is not None))
+                return out
+            return call
+
+    monkeypatch.setattr(mxp, "_fast", Noting())
+    got = calls()
+    if not isinstance(native, mxp._NoNative):
+        assert len(taken) == 9 and all(ok for _, ok in taken), taken
+    monkeypatch.setattr(mxp, "_fast", mxp._NoNative())
+    for a, w_ in zip(got, calls()):
+        assert a.dtype == w_.dtype and torch.equal(a.view(torch.uint8) if a.dtype == torch.uint8 else a, w_)
+
+
 class Layer:
     """The attention half of a layer as a serving program runs it: norm, joint projection, cache, attention, next residual."""
 
