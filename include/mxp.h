@@ -399,7 +399,7 @@ int mxp_cache_read(const void* cache, int64_t n_pages, int64_t page_tokens, int6
  * workspace: mxp_attention_workspace_bytes(...) of the same arguments (may be 0), scratch for the parts of split sequences, free
  * again after the call's work on `stream`; a smaller one returns MXP_ERR_WORKSPACE. */
 size_t mxp_attention_workspace_bytes(int64_t n_seq, int64_t rows, int64_t max_q, int64_t max_kv, int64_t heads, int64_t kv_heads,
-                                     int64_t head_dim, int64_t window);
+                                     int64_t head_dim, int causal, int64_t window);
 int mxp_attention(const void* Q, int q_dtype, int64_t ld_q, int64_t rows, int64_t heads, const int32_t* q_start, const int32_t* kv_len,
                   const int32_t* table, int64_t ld_table, int64_t n_seq, int64_t max_q, int64_t max_kv, float scale, int causal,
                   int64_t window, const void* cache, int64_t n_pages, int64_t page_tokens, int64_t kv_heads, int64_t head_dim, int fmt,

@@ -14,7 +14,7 @@
 // Query rows of one key-value head (heads that share it x queries) are taken together.  attn_few_kernel: up to 32 of them per
 // workgroup, every wavefront with tokens of its own, joined through LDS at the end; bound by reading the cache.
 // attn_many_kernel: 128 rows per workgroup, the wavefronts share the de-converted tokens; bound by the matrix cores and the softmax.
-// Both can split a sequence's tokens over workgroups; a second kernel then joins the parts.
+// Both can deal a sequence's tokens out to several workgroups; attn_join_kernel then joins the parts.
 #include "mxp_cache.h"
 
 namespace {
@@ -51,9 +51,10 @@ struct AttnArgs {
   int o_bf16;
   float *lse, *part_o, *part_ml;                             // parts of rows: D values, maximum and sum
   int32_t* joins;                                            // few rows: [workgroup][4], see Share
-  int direct, splits, chunk, row_tiles;
+  int direct, row_tiles;
 };
 
+constexpr int kWaves = 4;                                     // of a workgroup
 constexpr float kInf = __builtin_inff();
 __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ float zero_if_none(float m) { return m == -kInf ? 0.0f : m; }   // 2^(x - m) where nothing was seen yet
@@ -138,17 +139,13 @@ struct Sequence {
   }
 };
 
-// The tokens that a tile of rows and one split go over: [begin, end), begin a multiple of 32
+// The tokens [begin, end) that any of `rows` > 0 rows from `row` on sees, begin a multiple of 32
 struct Span {
-  int begin, end;
-  __device__ __forceinline__ Span(int b, int e) : begin(b), end(e) {}
-  __device__ __forceinline__ Span(const AttnArgs& a, const Sequence& s, int row, int rows, int split) {   // rows > 0
-    const int i0 = row / a.group, i1 = (row + rows - 1) / a.group;
-    const int hi = s.last(a, i1) + 1, lo = s.first(a, i0) & ~31;
-    const int64_t b = lo + (int64_t)split * a.chunk;
-    begin = b < hi ? (int)b : hi;
-    end = split + 1 < a.splits && b + a.chunk < hi ? (int)b + a.chunk : hi;
-    if (end < begin) end = begin;
+  int begin = 0, end = 0;
+  Span() = default;
+  __device__ __forceinline__ Span(const AttnArgs& a, const Sequence& s, int row, int rows) {
+    begin = s.first(a, row / a.group) & ~31;
+    end = s.last(a, (row + rows - 1) / a.group) + 1;
   }
 };
 
@@ -222,33 +219,157 @@ __device__ __forceinline__ void store_out(const AttnArgs& a, int64_t row, int he
   else *reinterpret_cast<f32x4*>(static_cast<float*>(a.o) + off) = v;
 }
 
-// The end of a row: the output itself, or this split's part of it
-__device__ __forceinline__ void finish_values(const AttnArgs& a, int split, int64_t row, int head, int d, f32x4 v, float l) {
-  if (a.splits == 1) store_out(a, row, head, d, l == 0.0f ? f32x4{0, 0, 0, 0} : v / l);
-  else *reinterpret_cast<f32x4*>(a.part_o + (((int64_t)split * a.rows + row) * a.heads + head) * a.g.D + d) = v;
-}
 __device__ __forceinline__ float lse_of(float m, float l) { return l == 0.0f ? -kInf : (m + __builtin_amdgcn_logf(l)) * 0.69314718055994531f; }
-__device__ __forceinline__ void finish_row(const AttnArgs& a, int split, int64_t row, int head, float m, float l) {
-  if (a.splits > 1) {
-    float* p = a.part_ml + (((int64_t)split * a.rows + row) * a.heads + head) * 2;
-    p[0] = m;
-    p[1] = l;
+// The end of a row: the output itself, or a part of it
+__device__ __forceinline__ void finish_values(const AttnArgs& a, int64_t part_row, int64_t row, int head, int d, f32x4 v, float l) {
+  if (part_row < 0) store_out(a, row, head, d, l == 0.0f ? f32x4{0, 0, 0, 0} : v / l);
+  else *reinterpret_cast<f32x4*>(a.part_o + part_row * a.g.D + d) = v;
+}
+__device__ __forceinline__ void finish_row(const AttnArgs& a, int64_t part_row, int64_t row, int head, float m, float l) {
+  if (part_row >= 0) {
+    a.part_ml[2 * part_row] = m;
+    a.part_ml[2 * part_row + 1] = l;
   } else if (a.lse) {
     a.lse[row * a.heads + head] = lse_of(m, l);
   }
 }
 
-// The work of a workgroup: split fastest, then tile of rows, key-value head, sequence
-struct Work {
-  int split, tile, head, seq;
-  __device__ __forceinline__ explicit Work(const AttnArgs& a) {
-    uint32_t id = blockIdx.x;
-    split = (int)(id % (uint32_t)a.splits);
-    id /= (uint32_t)a.splits;
-    tile = (int)(id % (uint32_t)a.row_tiles);
-    id /= (uint32_t)a.row_tiles;
-    head = (int)(id % (uint32_t)a.g.kv_heads);
-    seq = (int)(id / (uint32_t)a.g.kv_heads);
+// ---- dealing out the work --------------------------------------------------------------------------------------------
+// How a call's work is dealt to workgroups where it is split: in units of tokens, counted over sequences, their key-value heads and
+// their tiles of rows.  Workgroup g of n takes units [g total / n, (g + 1) total / n), whatever
+// the lengths are: a run of rows' tokens that begins or ends inside one (seq, head, tile).  Those two leave parts in the workspace, at
+// 2 g (begun by another workgroup) and 2 g + 1 (begun here); what lies between them is finished here.  The workgroup that begins
+// rows that others go on with records so, and attn_join_kernel adds the parts of its workgroup and of those behind it.
+struct Load {
+  int first, end, units, tiles;                              // tokens that any row sees, in units; tiles of rows
+  int64_t total;                                             // units x tiles x key-value heads
+  __device__ __forceinline__ Load(const AttnArgs& a, const Sequence& s, int rows, int unit) {
+    first = end = 0;
+    if (s.n > 0) {
+      first = s.first(a, 0) & ~31;
+      end = s.last(a, s.n - 1) + 1;
+    }
+    units = end > first ? (end - first + unit - 1) / unit : 1;   // (rows that see nothing are written too)
+    tiles = (s.n * a.group + rows - 1) / rows;
+    total = (int64_t)units * tiles * a.g.kv_heads;
+  }
+};
+struct Share {
+  int64_t begin, end, total;                                 // this workgroup's units; all
+  int seq, item, off, n;                                     // where `begin` is: sequence, item in it, unit of the item; workgroups that have any
+  __device__ __forceinline__ int workgroup_of(int64_t unit) const { return (int)(((unit + 1) * n - 1) / total); }
+};
+__device__ __forceinline__ void find_share(const AttnArgs& a, int rows, int unit, int least, Share& share, int64_t (&wave_sum)[kWaves]) {
+  const int each = (a.n_seq + 64 * kWaves - 1) / (64 * kWaves), lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int s0 = (int)threadIdx.x * each, s1 = s0 + each < a.n_seq ? s0 + each : a.n_seq;
+  int64_t mine = 0;
+  for (int s = s0; s < s1; ++s) mine += Load(a, Sequence(a, s), rows, unit).total;
+  int64_t upto = mine;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int64_t x = __shfl_up(upto, d);
+    upto += lane >= d ? x : 0;
+  }
+  if (lane == 63) wave_sum[wave] = upto;
+  if (threadIdx.x == 0) {                                    // (what a workgroup without a share finds)
+    share.begin = share.end = share.total = 0;
+    share.seq = share.item = share.off = share.n = 0;
+  }
+  __syncthreads();
+  int64_t total = 0;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    if (w < wave) upto += wave_sum[w];
+    total += wave_sum[w];
+  }
+  const int64_t most = (total + least - 1) / least;
+  const int64_t n = most < (int64_t)gridDim.x ? most : (int64_t)gridDim.x;
+  if ((int64_t)blockIdx.x < n) {
+    const int64_t begin = blockIdx.x * total / n, end = (blockIdx.x + 1) * total / n;
+    int64_t before = upto - mine;
+    if (begin >= before && begin < upto)                     // one lane: the sequence is one of its own
+      for (int s = s0; s < s1; ++s) {
+        const Load load(a, Sequence(a, s), rows, unit);
+        if (begin < before + load.total) {
+          share.begin = begin;
+          share.end = end;
+          share.total = total;
+          share.seq = s;
+          share.item = (int)((begin - before) / load.units);
+          share.off = (int)((begin - before) % load.units);
+          share.n = (int)n;
+          break;
+        }
+        before += load.total;
+      }
+  }
+  __syncthreads();
+}
+
+// The rows and tokens that a workgroup goes over, one run after another: its share, or (a.direct) whole tiles of rows.
+struct Walk {
+  int seq, kv_head = 0, tile = 0, item = 0, off = 0;
+  int64_t left = 0, end = 0;
+  int part = -1;                                             // where a run's result goes: out, or among the parts
+  __device__ __forceinline__ Walk(const AttnArgs& a, int rows, int unit, int least, Share& share, int64_t (&wave_sum)[kWaves]) {
+    if (a.direct) {
+      uint32_t id = blockIdx.x;                              // tile of rows fastest, then key-value head, then sequence
+      tile = (int)(id % (uint32_t)a.row_tiles);
+      id /= (uint32_t)a.row_tiles;
+      kv_head = (int)(id % (uint32_t)a.g.kv_heads);
+      seq = (int)(id / (uint32_t)a.g.kv_heads);
+    } else {
+      find_share(a, rows, unit, least, share, wave_sum);
+      if (threadIdx.x == 0) a.joins[4 * blockIdx.x] = -1;
+      end = uniform(share.end);
+      left = end - uniform(share.begin);
+      seq = uniform(share.seq);
+      item = uniform(share.item);
+      off = uniform(share.off);
+    }
+  }
+  // whether there is more to do; `seq` is a sequence's number only then
+  __device__ __forceinline__ bool more(const AttnArgs& a) const { return a.direct || (left > 0 && seq < a.n_seq); }
+  __device__ __forceinline__ bool more(const AttnArgs& a, const Sequence& s, int rows) const { return !a.direct || tile * rows < s.n * a.group; }
+  // The next run: its tile of rows and span of tokens.  False where the sequence has none left (the next one may).
+  __device__ __forceinline__ bool next(const AttnArgs& a, const Sequence& s, int rows, int unit, const Share& share, int& r0, Span& span) {
+    const int R = s.n * a.group;
+    int from = 0, to = 0x7FFFFFFF;
+    if (a.direct) {
+      const int tiles = (R + rows - 1) / rows;
+      r0 = (tiles - 1 - tile) * rows;                        // the last rows see most: they start first
+      tile += a.row_tiles;
+    } else {
+      const Load load(a, s, rows, unit);
+      if (item >= load.tiles * a.g.kv_heads) {
+        ++seq;
+        item = 0;
+        return false;
+      }
+      const int till = left < load.units - off ? off + (int)left : load.units;
+      kv_head = item / load.tiles;
+      r0 = (item - kv_head * load.tiles) * rows;
+      from = load.first + off * unit;
+      if (till < load.units) to = load.first + till * unit;
+      part = -1;
+      if (off > 0 || till < load.units) {
+        part = 2 * (int)blockIdx.x + (off == 0 ? 1 : 0);
+        if (off == 0 && threadIdx.x == 0) {                  // the first part of these rows: the join goes on to the last one's workgroup
+          int32_t* const j = a.joins + 4 * blockIdx.x;
+          j[1] = kv_head;
+          j[2] = r0;
+          j[3] = share.workgroup_of(end - left + load.units - 1);
+          j[0] = seq;
+        }
+      }
+      left -= till - off;
+      off = 0;
+      ++item;
+    }
+    span = Span(a, s, r0, R - r0 < rows ? R - r0 : rows);
+    if (span.begin < from) span.begin = from;
+    if (span.end > to) span.end = to;
+    return true;
   }
 };
 
@@ -356,151 +477,40 @@ __device__ __forceinline__ void join_row_by_wave(const AttnArgs& a, int parts, P
 }
 
 // ---- few rows -------------------------------------------------------------------------------------------------------
-constexpr int kFewWaves = 4, kFewAhead = 1;                   // tiles in flight per wavefront
+constexpr int kFewUnit = 32 * kWaves, kFewLeast = 4;          // tokens (a 32-token tile per wavefront); units per workgroup at least
+constexpr int kFewAhead = 1;                   // tiles in flight per wavefront
 template <int D>
 constexpr int few_pitch() { return 2 * D + 16; }             // bytes per token: 16 rows' 16-byte reads fall on all banks
 template <int D>
 constexpr int few_patch(int nt) { return 32 * few_pitch<D>() > 16 * nt * D * 4 ? 32 * few_pitch<D>() : 16 * nt * D * 4; }
 template <int D>
-constexpr int few_lds(int nt) { return kFewWaves * (few_patch<D>(nt) + 16 * nt * 8); }
+constexpr int few_lds(int nt) { return kWaves * (few_patch<D>(nt) + 16 * nt * 8); }
 constexpr int few_waves_per_simd(int D, int NT) { return D * NT <= 128 ? 4 : D * NT <= 256 ? 2 : 1; }
-
-// How a call's work is dealt to workgroups where it is split: in units of 128 tokens (a 32-token tile per wavefront), counted over
-// sequences, their key-value heads and their tiles of rows.  Workgroup g of n takes units [g total / n, (g + 1) total / n), whatever
-// the lengths are: a run of rows' tokens that begins or ends inside one (seq, head, tile).  Those two leave parts in the workspace, at
-// 2 g (begun by another workgroup) and 2 g + 1 (begun here); what lies between them is finished here.  The workgroup that begins
-// rows that others go on with records so, and attn_few_join_kernel adds the parts of its workgroup and of those behind it.
-constexpr int kUnit = 32 * kFewWaves, kLeastUnits = 4;       // at least so many units per workgroup
-struct Load {
-  int first, end, units, tiles;                              // tokens that any row sees, in units; tiles of rows
-  int64_t total;                                             // units x tiles x key-value heads
-  __device__ __forceinline__ Load(const AttnArgs& a, const Sequence& s, int rows) {
-    first = end = 0;
-    if (s.n > 0) {
-      first = s.first(a, 0) & ~31;
-      end = s.last(a, s.n - 1) + 1;
-    }
-    units = end > first ? (end - first + kUnit - 1) / kUnit : 1;   // (rows that see nothing are written too)
-    tiles = (s.n * a.group + rows - 1) / rows;
-    total = (int64_t)units * tiles * a.g.kv_heads;
-  }
-};
-struct Share {
-  int64_t begin, end, total;                                 // this workgroup's units; all
-  int seq, item, off, n;                                     // where `begin` is: sequence, item in it, unit of the item; workgroups that have any
-  __device__ __forceinline__ int workgroup_of(int64_t unit) const { return (int)(((unit + 1) * n - 1) / total); }
-};
-__device__ __forceinline__ void find_share(const AttnArgs& a, int rows, Share& share, int64_t (&wave_sum)[kFewWaves]) {
-  const int each = (a.n_seq + 64 * kFewWaves - 1) / (64 * kFewWaves), lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int s0 = (int)threadIdx.x * each, s1 = s0 + each < a.n_seq ? s0 + each : a.n_seq;
-  int64_t mine = 0;
-  for (int s = s0; s < s1; ++s) mine += Load(a, Sequence(a, s), rows).total;
-  int64_t upto = mine;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const int64_t x = __shfl_up(upto, d);
-    upto += lane >= d ? x : 0;
-  }
-  if (lane == 63) wave_sum[wave] = upto;
-  if (threadIdx.x == 0) share.begin = share.end = 0;
-  __syncthreads();
-  int64_t total = 0;
-#pragma unroll
-  for (int w = 0; w < kFewWaves; ++w) {
-    if (w < wave) upto += wave_sum[w];
-    total += wave_sum[w];
-  }
-  const int64_t most = (total + kLeastUnits - 1) / kLeastUnits;
-  const int64_t n = most < (int64_t)gridDim.x ? most : (int64_t)gridDim.x;
-  if ((int64_t)blockIdx.x < n) {
-    const int64_t begin = blockIdx.x * total / n, end = (blockIdx.x + 1) * total / n;
-    int64_t before = upto - mine;
-    if (begin >= before && begin < upto)                     // one lane: the sequence is one of its own
-      for (int s = s0; s < s1; ++s) {
-        const Load load(a, Sequence(a, s), rows);
-        if (begin < before + load.total) {
-          share.begin = begin;
-          share.end = end;
-          share.total = total;
-          share.seq = s;
-          share.item = (int)((begin - before) / load.units);
-          share.off = (int)((begin - before) % load.units);
-          share.n = (int)n;
-          break;
-        }
-        before += load.total;
-      }
-  }
-  __syncthreads();
-}
 
 // NT tiles of 16 rows; TERMS: bf16 terms of P
 template <int D, int MODE, int NT, int TERMS>
-__global__ void __launch_bounds__(64 * kFewWaves, few_waves_per_simd(D, NT)) attn_few_kernel(const AttnArgs a) {
+__global__ void __launch_bounds__(64 * kWaves, few_waves_per_simd(D, NT)) attn_few_kernel(const AttnArgs a) {
   constexpr int DB = D / 32, NB = D / 64, PITCH = few_pitch<D>(), PATCH = few_patch<D>(NT);   // blocks per token; per lane of a 32-token tile
   constexpr int LANE_TOKENS = D == 64 ? 32 : 16;             // tokens that a wavefront's lanes cover with one block each (of 2, 4, 4 neighbours)
   extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 15, quarter = lane >> 4;
   uint8_t* const patch = lds + wave * PATCH;                 // a tile's keys, then its values
-  float* const ml = reinterpret_cast<float*>(lds + kFewWaves * PATCH);   // [wave][row][2]
+  float* const ml = reinterpret_cast<float*>(lds + kWaves * PATCH);   // [wave][row][2]
   // this lane's blocks of a tile: its token (16 lanes in a row have 16 tokens: their stores fall on all banks), its block of the token
   const auto token_of = [&](int i) { return D == 256 ? 16 * (i >> 1) + (lane & 15) : LANE_TOKENS * i + (lane & (LANE_TOKENS - 1)); };
   const auto block_of = [&](int i) { return D == 256 ? 4 * (i & 1) + (lane >> 4) : lane / LANE_TOKENS; };
-  // What to do: rows r0 ... of one key-value head of a sequence, over a span of its tokens
   constexpr int ROWS = 16 * NT;
   __shared__ Share share;
-  __shared__ int64_t wave_sum[kFewWaves];
-  int seq, kv_head = 0, tile = 0, item = 0, off = 0;
-  int64_t left = 0;                                          // units; not used where a workgroup has whole items (a.direct)
-  if (a.direct) {
-    const Work w(a);
-    seq = w.seq;
-    kv_head = w.head;
-    tile = w.tile;
-  } else {
-    find_share(a, ROWS, share, wave_sum);
-    if (threadIdx.x == 0) a.joins[4 * blockIdx.x] = -1;
-    left = uniform(share.end) - uniform(share.begin);
-    if (left == 0) return;
-    seq = uniform(share.seq);
-    item = uniform(share.item);
-    off = uniform(share.off);
-  }
-  for (;;) {
-    const Sequence s(a, seq);
-    const int R = s.n * a.group;
-    Span span(0, 0);
-    int part = -1;                                           // where the result goes: out, or among the parts
-    if (a.direct) {
-      if (tile * ROWS >= R) break;
-      span = Span(a, s, tile * ROWS, R - tile * ROWS < ROWS ? R - tile * ROWS : ROWS, 0);
-    } else {
-      const Load load(a, s, ROWS);
-      if (item >= load.tiles * a.g.kv_heads) {               // on to the next sequence
-        ++seq;
-        item = 0;
-        continue;
-      }
-      const int till = left < load.units - off ? off + (int)left : load.units;
-      kv_head = item / load.tiles;
-      tile = item - kv_head * load.tiles;
-      span = Span(load.first + off * kUnit, till == load.units ? load.end : load.first + till * kUnit);
-      if (off > 0 || till < load.units) {
-        part = 2 * (int)blockIdx.x + (off == 0 ? 1 : 0);
-        if (off == 0 && threadIdx.x == 0) {                  // the first part of these rows: the join goes on to the last one's workgroup
-          int32_t* const j = a.joins + 4 * blockIdx.x;
-          j[1] = kv_head;
-          j[2] = tile * ROWS;
-          j[3] = share.workgroup_of(share.end - left + load.units - 1);
-          j[0] = seq;
-        }
-      }
-      left -= till - off;
-      off = 0;
-      ++item;
-    }
-    const int r0 = tile * ROWS;
+  __shared__ int64_t wave_sum[kWaves];
+  for (Walk walk(a, ROWS, kFewUnit, kFewLeast, share, wave_sum);;) {
+    if (!walk.more(a)) break;
+    const Sequence s(a, walk.seq);
+    if (!walk.more(a, s, ROWS)) break;
+    int r0 = 0;
+    Span span;
+    if (!walk.next(a, s, ROWS, kFewUnit, share, r0, span)) continue;
+    const int R = s.n * a.group, kv_head = walk.kv_head, part = walk.part;
     // this lane's rows, as operands of the first product: channels 32 st + 8 quarter ... + 7
     Operand q[NT][DB];
     int first[NT], last[NT];
@@ -529,7 +539,7 @@ __global__ void __launch_bounds__(64 * kFewWaves, few_waves_per_simd(D, NT)) att
 #pragma unroll
       for (int d = 0; d < D / 16; ++d) o[t][d] = f32x4{0, 0, 0, 0};
     }
-    // The wavefront's tiles: span.begin + 32 wave, and every 32 kFewWaves tokens from there.  Lane n holds the page of half n % 2 of
+    // The wavefront's tiles: span.begin + 32 wave, and every 32 kWaves tokens from there.  Lane n holds the page of half n % 2 of
     // tile n / 2 of the next 32 tiles (-1: none), so that a tile's addresses wait for no table.
     const int begin = span.begin + 32 * wave;
     int fetched = 0;                                         // tiles
@@ -540,7 +550,7 @@ __global__ void __launch_bounds__(64 * kFewWaves, few_waves_per_simd(D, NT)) att
     } ahead[kFewAhead];
     const auto fetch = [&](Fetched& f, int t) {
       if (t >= span.end) return;
-      if ((fetched & 31) == 0) pages = page_of(a, s, (int64_t)t + 32 * kFewWaves * (lane >> 1) + 16 * (lane & 1));
+      if ((fetched & 31) == 0) pages = page_of(a, s, (int64_t)t + 32 * kWaves * (lane >> 1) + 16 * (lane & 1));
       const Page p0(a, kv_head, __builtin_amdgcn_readlane(pages, 2 * (fetched & 31)), t), p1(a, kv_head, __builtin_amdgcn_readlane(pages, 2 * (fetched & 31) + 1), t + 16);
       f.held0 = p0.held;
       f.held1 = p1.held;
@@ -588,7 +598,7 @@ __global__ void __launch_bounds__(64 * kFewWaves, few_waves_per_simd(D, NT)) att
         expand<MODE>(f.v[i], dead || f.v[i].scale == 255u, patch + token * PITCH + block_of(i) * 64);
       }
       __builtin_amdgcn_wave_barrier();
-      fetch(f, t0 + kFewAhead * 32 * kFewWaves);
+      fetch(f, t0 + kFewAhead * 32 * kWaves);
       const bool whole = h0 && h1 && t0 >= all_from && t0 + 31 <= all_to && t0 + 32 <= span.end;   // (uniform)
       if (!whole) {
 #pragma unroll
@@ -649,10 +659,10 @@ __global__ void __launch_bounds__(64 * kFewWaves, few_waves_per_simd(D, NT)) att
       __builtin_amdgcn_wave_barrier();
     };
 #pragma unroll
-    for (int u = 0; u < kFewAhead; ++u) fetch(ahead[u], begin + u * 32 * kFewWaves);
-    for (int t0 = begin; t0 < span.end; t0 += kFewAhead * 32 * kFewWaves)
+    for (int u = 0; u < kFewAhead; ++u) fetch(ahead[u], begin + u * 32 * kWaves);
+    for (int t0 = begin; t0 < span.end; t0 += kFewAhead * 32 * kWaves)
 #pragma unroll
-      for (int u = 0; u < kFewAhead; ++u) take(ahead[u], t0 + u * 32 * kFewWaves);
+      for (int u = 0; u < kFewAhead; ++u) take(ahead[u], t0 + u * 32 * kWaves);
     // join the wavefronts: each leaves its rows in its own patch
     float* const mine = reinterpret_cast<float*>(patch);
 #pragma unroll
@@ -666,42 +676,32 @@ __global__ void __launch_bounds__(64 * kFewWaves, few_waves_per_simd(D, NT)) att
       for (int d = 0; d < D / 16; ++d) *reinterpret_cast<f32x4*>(mine + (16 * t + col) * D + 16 * d + 4 * quarter) = o[t][d];
     }
     __syncthreads();
-    for (int j = threadIdx.x; j < 16 * NT * (D / 4); j += 64 * kFewWaves) {
+    for (int j = threadIdx.x; j < 16 * NT * (D / 4); j += 64 * kWaves) {
       const int row = j / (D / 4), d = (j - row * (D / 4)) * 4, r = r0 + row;
       if (r >= R) break;
       float top = -kInf, sum = 0.0f;
 #pragma unroll
-      for (int v = 0; v < kFewWaves; ++v) top = fmaxf(top, ml[(v * 16 * NT + row) * 2]);
+      for (int v = 0; v < kWaves; ++v) top = fmaxf(top, ml[(v * 16 * NT + row) * 2]);
       const float base = zero_if_none(top);
       f32x4 out = {0, 0, 0, 0};
 #pragma unroll
-      for (int v = 0; v < kFewWaves; ++v) {
+      for (int v = 0; v < kWaves; ++v) {
         const float f = exp2_of(ml[(v * 16 * NT + row) * 2] - base);
         sum += ml[(v * 16 * NT + row) * 2 + 1] * f;
         out += *reinterpret_cast<const f32x4*>(lds + v * PATCH + (row * D + d) * 4) * f;
       }
       const int i = r / a.group, head = kv_head * a.group + r - i * a.group;
-      if (part < 0) {
-        store_out(a, s.q0 + i, head, d, sum == 0.0f ? f32x4{0, 0, 0, 0} : out / sum);
-        if (d == 0 && a.lse) a.lse[(s.q0 + i) * a.heads + head] = lse_of(top, sum);
-      } else {
-        const int64_t at = (int64_t)part * 16 * NT + row;
-        *reinterpret_cast<f32x4*>(a.part_o + at * D + d) = out;
-        if (d == 0) {
-          a.part_ml[2 * at] = top;
-          a.part_ml[2 * at + 1] = sum;
-        }
-      }
+      const int64_t part_row = part < 0 ? -1 : (int64_t)part * ROWS + row;
+      finish_values(a, part_row, s.q0 + i, head, d, out, sum);
+      if (d == 0) finish_row(a, part_row, s.q0 + i, head, top, sum);
     }
     __syncthreads();
-    if (a.direct) tile += a.row_tiles;
-    else if (left == 0) break;
   }
 }
 
 // The joins that Share records, `each` workgroups' records per workgroup here: a row at a time by a wavefront, or by the workgroup
 // where the parts are many.
-__global__ void __launch_bounds__(256) attn_few_join_kernel(const AttnArgs a, int rows_per_tile, int n_records, int each) {
+__global__ void __launch_bounds__(256) attn_join_kernel(const AttnArgs a, int rows_per_tile, int n_records, int each) {
   __shared__ JoinRoom room;
   const int lane = threadIdx.x & 63, first = (int)blockIdx.x * each;
   uint64_t todo = __ballot(lane < each && first + lane < n_records && a.joins[4 * (first + lane)] >= 0);
@@ -722,34 +722,38 @@ __global__ void __launch_bounds__(256) attn_few_join_kernel(const AttnArgs a, in
 }
 
 // ---- many rows ------------------------------------------------------------------------------------------------------
-constexpr int kManyWaves = 4, kManyTokens = 64, kManyRows = 32 * kManyWaves;
+constexpr int kManyTokens = 64, kManyRows = 32 * kWaves, kManyLeast = 8;   // (a unit is a tile of tokens)
 template <int D>
 constexpr int many_pitch() { return 2 * D + 16; }
 template <int D>
 constexpr int many_buffers() { return D == 256 ? 1 : 2; }    // (two of D = 256 exceed the 160 KiB of a compute unit together with nothing else)
 template <int D>
-constexpr int many_lds() { return many_buffers<D>() * 2 * kManyTokens * many_pitch<D>() + 2 * kManyWaves * 2 * 4 * 8; }
+constexpr int many_lds() { return many_buffers<D>() * 2 * kManyTokens * many_pitch<D>() + 2 * kWaves * 2 * 4 * 8; }
 
 template <int D, int MODE, int TERMS>
-__global__ void __launch_bounds__(64 * kManyWaves) attn_many_kernel(const AttnArgs a) {
-  constexpr int DB = D / 32, NB = kManyTokens * DB / (64 * kManyWaves), PITCH = many_pitch<D>();
+__global__ void __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) attn_many_kernel(const AttnArgs a) {
+  constexpr int DB = D / 32, NB = kManyTokens * DB / (64 * kWaves), PITCH = many_pitch<D>();
   constexpr int BUF = many_buffers<D>(), HALF = kManyTokens * PITCH;
-  static_assert(NB * 64 * kManyWaves == kManyTokens * DB || D == 64, "blocks per lane");
+  static_assert(NB * 64 * kWaves == kManyTokens * DB || D == 64, "blocks per lane");
   constexpr int NL = NB < 1 ? 1 : NB;                        // D = 64: 128 blocks, the upper wavefronts have none
   extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
   uint64_t* const nans = reinterpret_cast<uint64_t*>(lds + BUF * 2 * HALF);   // [buffer][wave][NL] lanes with a NaN block of V
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 31, half = lane >> 5;
-  const Work w(a);
-  const Sequence s(a, w.seq);
-  const int R = s.n * a.group, tiles = (R + kManyRows - 1) / kManyRows;
-  for (int turn = w.tile; turn < tiles; turn += a.row_tiles) {
-    const int r0 = (tiles - 1 - turn) * kManyRows;           // the last rows see most: they start first
-    const Span span(a, s, r0, R - r0 < kManyRows ? R - r0 : kManyRows, w.split);
+  __shared__ Share share;
+  __shared__ int64_t wave_sum[kWaves];
+  for (Walk walk(a, kManyRows, kManyTokens, kManyLeast, share, wave_sum);;) {
+    if (!walk.more(a)) break;
+    const Sequence s(a, walk.seq);
+    if (!walk.more(a, s, kManyRows)) break;
+    int r0 = 0;
+    Span span;
+    if (!walk.next(a, s, kManyRows, kManyTokens, share, r0, span)) continue;
+    const int R = s.n * a.group, kv_head = walk.kv_head, part = walk.part;
     const int r = r0 + 32 * wave + col, i = r / a.group;
     const bool there = r < R;
     const int first = there ? s.first(a, i) : 1, last = there ? s.last(a, i) : 0;
-    const int head = w.head * a.group + (there ? r - i * a.group : 0);
+    const int head = kv_head * a.group + (there ? r - i * a.group : 0);
     Operand q[D / 16];
     {
       const uint16_t* p = a.q + (s.q0 + (there ? i : 0)) * a.ld_q + (int64_t)head * D + 8 * half;
@@ -782,7 +786,7 @@ __global__ void __launch_bounds__(64 * kManyWaves) attn_many_kernel(const AttnAr
       int at[4];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const Page p(a, w.head, __builtin_amdgcn_readlane(pages, 4 * (fetched & 15) + j), t + 16 * j);
+        const Page p(a, kv_head, __builtin_amdgcn_readlane(pages, 4 * (fetched & 15) + j), t + 16 * j);
         held_next |= (p.held ? 1u : 0u) << j;
         rec[j] = p.rec;
         at[j] = p.at;
@@ -790,7 +794,7 @@ __global__ void __launch_bounds__(64 * kManyWaves) attn_many_kernel(const AttnAr
       ++fetched;
 #pragma unroll
       for (int k = 0; k < NL; ++k) {
-        const int n = (int)threadIdx.x + 64 * kManyWaves * k, token = n / DB;
+        const int n = (int)threadIdx.x + 64 * kWaves * k, token = n / DB;
         if (token < kManyTokens) {
           const int j = token >> 4;
           const uint8_t* base = j & 2 ? (j & 1 ? rec[3] : rec[2]) : (j & 1 ? rec[1] : rec[0]);
@@ -804,7 +808,7 @@ __global__ void __launch_bounds__(64 * kManyWaves) attn_many_kernel(const AttnAr
       uint8_t* const kt = lds + buf * 2 * HALF;
 #pragma unroll
       for (int k = 0; k < NL; ++k) {
-        const int n = (int)threadIdx.x + 64 * kManyWaves * k, token = n / DB;
+        const int n = (int)threadIdx.x + 64 * kWaves * k, token = n / DB;
         bool bad = false;
         if (token < kManyTokens) {
           const bool dead = t + token >= span.end || !((held_next >> (token >> 4)) & 1u);
@@ -813,7 +817,7 @@ __global__ void __launch_bounds__(64 * kManyWaves) attn_many_kernel(const AttnAr
           expand<MODE>(vb[k], dead || bad, kt + HALF + token * PITCH + (n % DB) * 64);
         }
         const uint64_t b = __ballot(bad);
-        if (lane == 0) nans[(buf * kManyWaves + wave) * NL + k] = b;
+        if (lane == 0) nans[(buf * kWaves + wave) * NL + k] = b;
       }
     };
     int buf = 0;
@@ -885,11 +889,11 @@ __global__ void __launch_bounds__(64 * kManyWaves) attn_many_kernel(const AttnAr
         }
         uint64_t any = 0;
 #pragma unroll
-        for (int k = 0; k < kManyWaves * NL; ++k) any |= nans[buf * kManyWaves * NL + k];
+        for (int k = 0; k < kWaves * NL; ++k) any |= nans[buf * kWaves * NL + k];
         if (__any(any != 0)) {                               // NaN blocks of V, for the rows that see them
-          for (int k = 0; k < kManyWaves * NL; ++k)
-            for (uint64_t left = nans[buf * kManyWaves * NL + k]; left; left &= left - 1) {
-              const int n = __builtin_ctzll(left) + 64 * (k / NL) + 64 * kManyWaves * (k % NL), tok = t0 + n / DB;
+          for (int k = 0; k < kWaves * NL; ++k)
+            for (uint64_t left = nans[buf * kWaves * NL + k]; left; left &= left - 1) {
+              const int n = __builtin_ctzll(left) + 64 * (k / NL) + 64 * kWaves * (k % NL), tok = t0 + n / DB;
               if (tok >= first && tok <= last) {
 #pragma unroll
                 for (int d = 0; d < DB; ++d)
@@ -908,92 +912,65 @@ __global__ void __launch_bounds__(64 * kManyWaves) attn_many_kernel(const AttnAr
     }
     l = sum_across_32(l);
     if (there) {
+      const int64_t part_row = part < 0 ? -1 : (int64_t)part * kManyRows + 32 * wave + col;
 #pragma unroll
       for (int d = 0; d < DB; ++d)
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-          finish_values(a, w.split, s.q0 + i, head, 32 * d + 8 * j + 4 * half, f32x4{o[d][4 * j], o[d][4 * j + 1], o[d][4 * j + 2], o[d][4 * j + 3]}, l);
-      if (half == 0) finish_row(a, w.split, s.q0 + i, head, m * a.scale, l);
+          finish_values(a, part_row, s.q0 + i, head, 32 * d + 8 * j + 4 * half, f32x4{o[d][4 * j], o[d][4 * j + 1], o[d][4 * j + 2], o[d][4 * j + 3]}, l);
+      if (half == 0) finish_row(a, part_row, s.q0 + i, head, m * a.scale, l);
     }
     __syncthreads();
-  }
-}
-
-// ---- the parts of split sequences: many rows ---------------------------------------------------------------------------
-// Parts [split][row][head].  Rows that no sequence has are left as they are.
-__global__ void __launch_bounds__(256) attn_many_join_kernel(const AttnArgs a) {
-  __shared__ JoinRoom room;
-  const int64_t from = a.q_start ? a.q_start[0] : 0, to = a.q_start ? a.q_start[a.n_seq] : a.rows, n = a.rows * a.heads;
-  for (int64_t j = blockIdx.x; j < n; j += gridDim.x) {
-    const int64_t row = j / a.heads;
-    if (row >= from && row < to) join_row(a, room, a.splits, [&](int p) { return p * n + j; }, row, (int)(j - row * a.heads));
   }
 }
 
 // ---- launch -----------------------------------------------------------------------------------------------------------
 struct Plan {
   bool many, direct;
-  int nt, row_tiles, splits, chunk;
+  int rows, row_tiles;                                       // of a tile, tiles per key-value head and sequence
   int64_t wgs;
 };
 
 // Sequences of at most so many tokens are not dealt out in parts: a workgroup goes over them in less than the parts' join takes.
-constexpr int64_t kDirectTokens = 2048;
+constexpr int64_t kFewDirect = 2048, kManyDirect = 1024;
 
-// Which kernel, and how a sequence's tokens are dealt to workgroups.  Up to 32 rows of a key-value head: attn_few_kernel.
-Plan plan_for(int64_t n_seq, int64_t max_q, int64_t max_kv, int64_t heads, int64_t kv_heads, int64_t D, int64_t window) {
+// Which kernel (up to 32 rows of a key-value head: attn_few_kernel), and whether a workgroup takes whole tiles of rows or a share of
+// all tokens.  Whole tiles where sequences are short, where workgroups come in several rounds anyhow (they then even out among
+// themselves), and for prompts: a tile of theirs sees half the tokens on average, which shares of equal numbers of tokens do not heed.
+Plan plan_for(int64_t n_seq, int64_t max_q, int64_t max_kv, int64_t heads, int64_t kv_heads, int64_t D, int causal, int64_t window) {
   Plan p;
   const int64_t rows = max_q * (heads / kv_heads);           // of one key-value head
   p.many = rows > 32;
-  p.nt = rows > 16 ? 2 : 1;
-  const int64_t tile = p.many ? kManyRows : 16 * p.nt;
-  p.row_tiles = (int)((rows + tile - 1) / tile);
+  p.rows = p.many ? kManyRows : rows > 16 ? 32 : 16;
+  p.row_tiles = (int)((rows + p.rows - 1) / p.rows);
   if (p.row_tiles < 1) p.row_tiles = 1;
   const int64_t items = n_seq * kv_heads * p.row_tiles;
   int64_t len = max_kv;                                      // tokens that one tile of rows goes over, at most
   if (window > 0 && window + max_q + 32 < len) len = window + max_q + 32;
-  p.direct = false;
-  p.splits = 1;
-  p.chunk = 1 << 30;
-  p.wgs = items;
-  if (!p.many) {
-    const int64_t room = (int64_t)kNumCU * few_waves_per_simd((int)D, p.nt), units = items * ((len + kUnit - 1) / kUnit);
-    p.direct = len <= kDirectTokens || items >= 4 * room;
-    if (!p.direct) p.wgs = units < kLeastUnits * room ? (units + kLeastUnits - 1) / kLeastUnits : room;
-    return p;
-  }
-  const int64_t least = 512, want = 1024;                    // tokens per workgroup at least; workgroups wanted
-  int64_t splits = items < want ? (want + items - 1) / items : 1;
-  if (splits > (len + least - 1) / least) splits = (len + least - 1) / least;
-  if (splits < 1) splits = 1;
-  const int64_t chunk = ((len + splits - 1) / splits + kManyTokens - 1) / kManyTokens * kManyTokens;
-  p.chunk = (int)(chunk < kManyTokens ? kManyTokens : chunk > (1 << 30) ? (1 << 30) : chunk);
-  p.splits = (int)((len + p.chunk - 1) / p.chunk);
-  if (p.splits < 1) p.splits = 1;
-  p.wgs = items * p.splits;
+  const int64_t room = (int64_t)kNumCU * (p.many ? (D == 256 ? 1 : 2) : few_waves_per_simd((int)D, p.rows / 16));   // workgroups that run at once
+  const int64_t unit = p.many ? kManyTokens : kFewUnit, least = p.many ? kManyLeast : kFewLeast, units = items * ((len + unit - 1) / unit);
+  const bool prompt = p.many && causal && 2 * max_q > len && 2 * items > room;
+  p.direct = len <= (p.many ? kManyDirect : kFewDirect) || items >= 4 * room || prompt;
+  p.wgs = p.direct ? items : units < least * room ? (units + least - 1) / least : room;
   return p;
 }
 
 // Workspace: values of the parts, their maxima and sums, records of joins
-int64_t part_rows(const Plan& p, int64_t rows, int64_t heads) {
-  return p.many ? (p.splits > 1 ? p.splits * rows * heads : 0) : p.direct ? 0 : p.wgs * 2 * 16 * p.nt;
-}
-size_t parts_bytes(const Plan& p, int64_t rows, int64_t heads, int64_t D) {
-  return (size_t)part_rows(p, rows, heads) * (size_t)(D + 2) * 4 + (p.many || p.direct ? 0 : (size_t)p.wgs * 16);
-}
+int64_t part_rows(const Plan& p) { return p.direct ? 0 : p.wgs * 2 * p.rows; }
+size_t parts_bytes(const Plan& p, int64_t D) { return p.direct ? 0 : (size_t)part_rows(p) * (size_t)(D + 2) * 4 + (size_t)p.wgs * 16; }
 
 template <int D, int MODE, int TERMS>
 void launch(const AttnArgs& a, const Plan& p, hipStream_t s) {
   const dim3 grid((unsigned)p.wgs);
   if (p.many) {
     allow_dynamic_lds<attn_many_kernel<D, MODE, TERMS>>(many_lds<D>());
-    hipLaunchKernelGGL((attn_many_kernel<D, MODE, TERMS>), grid, dim3(64 * kManyWaves), many_lds<D>(), s, a);
-  } else if (p.nt == 2) {
+    hipLaunchKernelGGL((attn_many_kernel<D, MODE, TERMS>), grid, dim3(64 * kWaves), many_lds<D>(), s, a);
+  } else if (p.rows == 32) {
     allow_dynamic_lds<attn_few_kernel<D, MODE, 2, TERMS>>(few_lds<D>(2));
-    hipLaunchKernelGGL((attn_few_kernel<D, MODE, 2, TERMS>), grid, dim3(64 * kFewWaves), few_lds<D>(2), s, a);
+    hipLaunchKernelGGL((attn_few_kernel<D, MODE, 2, TERMS>), grid, dim3(64 * kWaves), few_lds<D>(2), s, a);
   } else {
     allow_dynamic_lds<attn_few_kernel<D, MODE, 1, TERMS>>(few_lds<D>(1));
-    hipLaunchKernelGGL((attn_few_kernel<D, MODE, 1, TERMS>), grid, dim3(64 * kFewWaves), few_lds<D>(1), s, a);
+    hipLaunchKernelGGL((attn_few_kernel<D, MODE, 1, TERMS>), grid, dim3(64 * kWaves), few_lds<D>(1), s, a);
   }
 }
 
@@ -1006,9 +983,9 @@ bool shapes_fit(int64_t n_seq, int64_t rows, int64_t max_q, int64_t max_kv, int6
 }  // namespace
 
 extern "C" size_t mxp_attention_workspace_bytes(int64_t n_seq, int64_t rows, int64_t max_q, int64_t max_kv, int64_t heads, int64_t kv_heads,
-                                                int64_t head_dim, int64_t window) {
+                                                int64_t head_dim, int causal, int64_t window) {
   if (!shapes_fit(n_seq, rows, max_q, max_kv, heads, kv_heads) || n_seq == 0 || rows == 0 || rows * heads > kMostRows || head_dim < 1 || window < 0) return 0;
-  return parts_bytes(plan_for(n_seq, max_q < rows ? max_q : rows, max_kv, heads, kv_heads, head_dim, window), rows, heads, head_dim);
+  return parts_bytes(plan_for(n_seq, max_q < rows ? max_q : rows, max_kv, heads, kv_heads, head_dim, causal, window), head_dim);
 }
 
 extern "C" int mxp_attention(const void* Q, int q_dtype, int64_t ld_q, int64_t rows, int64_t heads, const int32_t* q_start, const int32_t* kv_len,
@@ -1032,9 +1009,9 @@ extern "C" int mxp_attention(const void* Q, int q_dtype, int64_t ld_q, int64_t r
   if (!aligned16(Q) || !aligned16(O) || !aligned16(cache) || !aligned16(workspace) || ld_q * 2 % 16 != 0 || ld_o * osz % 16 != 0 || off4(q_start) ||
       off4(kv_len) || off4(table) || off4(lse))
     return MXP_ERR_ALIGN;
-  const Plan p = plan_for(n_seq, max_q < rows ? max_q : rows, max_kv, heads, kv_heads, head_dim, window);
+  const Plan p = plan_for(n_seq, max_q < rows ? max_q : rows, max_kv, heads, kv_heads, head_dim, causal, window);
   if (p.wgs > 2147483647LL) return MXP_ERR_UNSUPPORTED;
-  const size_t need = parts_bytes(p, rows, heads, head_dim);
+  const size_t need = parts_bytes(p, head_dim);
   if (need > 0 && (!workspace || workspace_bytes < need)) return MXP_ERR_WORKSPACE;
   a.q = static_cast<const uint16_t*>(Q);
   a.ld_q = ld_q;
@@ -1057,12 +1034,10 @@ extern "C" int mxp_attention(const void* Q, int q_dtype, int64_t ld_q, int64_t r
   a.o_bf16 = o_dtype == MXP_BF16;
   a.lse = lse;
   a.part_o = static_cast<float*>(workspace);
-  const size_t parts = (size_t)part_rows(p, rows, heads);
+  const size_t parts = (size_t)part_rows(p);
   a.part_ml = need ? a.part_o + parts * head_dim : nullptr;
   a.joins = need ? reinterpret_cast<int32_t*>(a.part_ml + 2 * parts) : nullptr;
   a.direct = p.direct ? 1 : 0;
-  a.splits = p.splits;
-  a.chunk = p.chunk;
   a.row_tiles = p.row_tiles;
   hipStream_t s = static_cast<hipStream_t>(stream);
 #define MXP_ATTN_T(D, M) do { if (a.o_bf16) launch<D, M, 1>(a, p, s); else launch<D, M, 3>(a, p, s); } while (0)
@@ -1072,17 +1047,14 @@ extern "C" int mxp_attention(const void* Q, int q_dtype, int64_t ld_q, int64_t r
   else MXP_ATTN_M(256);
 #undef MXP_ATTN_M
 #undef MXP_ATTN_T
-  if (p.many && p.splits > 1) {
-    const int64_t want = rows * heads;
-    hipLaunchKernelGGL(attn_many_join_kernel, dim3((unsigned)(want < (1 << 20) ? want : (1 << 20))), dim3(256), 0, s, a);
-  } else if (!p.many && !p.direct) {
+  if (!p.direct) {
     // Where many parts are to be joined there are few records: 16 of them and one row per workgroup (one sequence of 131000 tokens,
     // 8 joins of 128 parts: 14.6 -> 7.8 us against a record each); else a record per workgroup and a row per wavefront.
     int64_t most = (max_q < rows ? max_q : rows) * a.group;
-    most = most < 1 ? 1 : most < 16 * p.nt ? most : 16 * p.nt;
+    most = most < 1 ? 1 : most < p.rows ? most : p.rows;
     const bool many_parts = p.wgs > 32 * n_seq * kv_heads * p.row_tiles;
     const int each = many_parts ? 16 : 1;
-    hipLaunchKernelGGL(attn_few_join_kernel, dim3((unsigned)((p.wgs + each - 1) / each), (unsigned)(many_parts ? most : (most + 3) / 4)), dim3(256), 0, s, a, 16 * p.nt,
+    hipLaunchKernelGGL(attn_join_kernel, dim3((unsigned)((p.wgs + each - 1) / each), (unsigned)(many_parts ? most : (most + 3) / 4)), dim3(256), 0, s, a, p.rows,
                        (int)p.wgs, each);
   }
   return launch_status();

@@ -346,7 +346,7 @@ PyObject* fast_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (max_q < 0) max_q = start ? rows : 1;
   if (max_kv < 0) max_kv = std::min<int64_t>(table->size(1) * c.page, (int64_t)1 << 30);
   at::Tensor out = at::empty({rows, heads, c.D}, at::TensorOptions().dtype(d == MXP_BF16 ? at::kBFloat16 : at::kFloat).device(q->device())), ws;
-  const int64_t need = (int64_t)lib.attention_ws(seqs, rows, max_q, max_kv, heads, c.heads, c.D, window);
+  const int64_t need = (int64_t)lib.attention_ws(seqs, rows, max_q, max_kv, heads, c.heads, c.D, (int)causal, window);
   if (need > 0) ws = bytes(*q, {need});
   if (unlocked([&] {
         return lib.attention(q->data_ptr(), dtype_code(*q), ld3(*q), rows, heads, static_cast<const int32_t*>(data(start)), static_cast<const int32_t*>(len->data_ptr()),

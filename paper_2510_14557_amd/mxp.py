@@ -114,7 +114,7 @@ def lib():
     L.mxp_cache_bytes.restype = sz
     L.mxp_cache_write.argtypes = [vp, vp, i32, i64, i64, i64, vp, vp, i64, i64, i64, i64, i32, vp]
     L.mxp_cache_read.argtypes = [vp, i64, i64, i64, i64, i32, vp, i64, vp, vp, i32, i64, i64, vp]
-    L.mxp_attention_workspace_bytes.argtypes = [i64] * 8
+    L.mxp_attention_workspace_bytes.argtypes = [i64] * 7 + [i32, i64]
     L.mxp_attention_workspace_bytes.restype = sz
     L.mxp_attention.argtypes = ([vp, i32, i64, i64, i64, vp, vp, vp, i64, i64, i64, i64, C.c_float, i32, i64, vp, i64, i64, i64, i64, i32] +
                                 [vp, i32, i64, vp, vp, sz, vp])
@@ -710,8 +710,9 @@ def cache_read(cache: KVCache, slots: torch.Tensor, dtype: torch.dtype = torch.b
     return k, v
 
 
-def attention_workspace_bytes(n_seq: int, rows: int, max_q: int, max_kv: int, heads: int, kv_heads: int, head_dim: int, window: int = 0) -> int:
-    return int(lib().mxp_attention_workspace_bytes(n_seq, rows, max_q, max_kv, heads, kv_heads, head_dim, window))
+def attention_workspace_bytes(n_seq: int, rows: int, max_q: int, max_kv: int, heads: int, kv_heads: int, head_dim: int, causal: bool = True,
+                              window: int = 0) -> int:
+    return int(lib().mxp_attention_workspace_bytes(n_seq, rows, max_q, max_kv, heads, kv_heads, head_dim, int(causal), window))
 
 
 def attention(q: torch.Tensor, cache: KVCache, table: torch.Tensor, kv_len: torch.Tensor, q_start: torch.Tensor | None = None,
@@ -753,7 +754,7 @@ def attention(q: torch.Tensor, cache: KVCache, table: torch.Tensor, kv_len: torc
     if max_kv is None:
         max_kv = min(table.shape[1] * cache.page_tokens, 2 ** 30)
     if workspace is None:
-        nbytes = attention_workspace_bytes(n_seq, rows, max_q, max_kv, heads, cache.kv_heads, D, window)
+        nbytes = attention_workspace_bytes(n_seq, rows, max_q, max_kv, heads, cache.kv_heads, D, causal, window)
         workspace = torch.empty(nbytes, dtype=torch.uint8, device=q.device) if nbytes else None
     elif workspace.dtype != torch.uint8 or not workspace.is_contiguous():
         raise MxpError("workspace must be a contiguous uint8 tensor")
