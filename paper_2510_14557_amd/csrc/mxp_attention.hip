@@ -182,33 +182,53 @@ __device__ __forceinline__ Block load_block(const uint8_t* rec, const CacheGeom&
   return b;
 }
 
-// 32 bf16 at dst (16-byte aligned, in LDS).  A flushed block, or one to be left out (`drop`), becomes zeros; a scale byte of 255
-// makes the unpack-converts answer NaN (also for zero codes, so what is left out gets another).
+// Tokens in LDS: 2 D bytes each, without gaps, the 16-byte pieces of a token in an order of its own: piece c lies at c ^ s(token).
+// With s below the 16 pieces that 16 tokens have at the same channels fall on all banks (the stores of a de-converted block per
+// lane, the reads of K), and so do four neighbouring tokens' 64 bytes each (the transposed reads of V); rows padded to a pitch of
+// 2 D + 16 bytes left more than half of the LDS cycles to conflicts.  `at` is the token's place, a multiple of 2 D, with its s: the
+// piece at channel byte b (a multiple of 16) is at ^ b.
+template <int D>
+__device__ __forceinline__ uint32_t token_at(int token) {
+  const uint32_t t = (uint32_t)token;
+  const uint32_t s = D == 64 ? ((t & 2u) << 1) | (((t >> 2) & 3u) ^ ((t & 1u) << 1)) : ((t & 3u) << 2) | (((t >> 2) & 3u) ^ (t & 2u));
+  return t * (2u * D) | (s << 4);
+}
+
+// A place whose variants (^ b) are to be formed where they are used: kept in registers over the loop, they cost the few-row kernel its
+// fourth wavefront per SIMD (64 sequences of 8192 tokens: 151 us, and 135 so).
+__device__ __forceinline__ uint32_t formed_at_use(uint32_t at) {
+  asm volatile("" : "+v"(at));
+  return at;
+}
+
+// A block's 32 bf16 into LDS, its first byte at tile + at (`at` as above, with the block's channels).  A flushed block, or one to be
+// left out (`drop`), becomes zeros; a scale byte of 255 makes the unpack-converts answer NaN (also for zero codes, so what is left
+// out gets another).
 template <int MODE>
-__device__ __forceinline__ void expand(const Block& b, bool drop, uint8_t* dst) {
+__device__ __forceinline__ void expand(const Block& b, bool drop, uint8_t* tile, uint32_t at) {
   const bool zero = drop || b.scale == 0u;
   const uint32_t keep = zero ? 0u : 0xFFFFFFFFu;
   const float X = __uint_as_float((drop ? 127u : b.scale - (MODE == 2 ? b.index >> 5 : 0u)) << 23);
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
+  for (uint32_t j = 0; j < 4; ++j) {
     const uint32_t c = b.code[j] & keep;
     union { bf16x2 v; uint32_t u; } w0, w1, w2, w3;
     w0.v = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, X, 0);
     w1.v = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, X, 1);
     w2.v = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, X, 2);
     w3.v = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, X, 3);
-    reinterpret_cast<u32x4*>(dst)[j] = u32x4{w0.u, w1.u, w2.u, w3.u};
+    *reinterpret_cast<u32x4*>(tile + (at ^ (16u * j))) = u32x4{w0.u, w1.u, w2.u, w3.u};
   }
   if (MODE >= 1) {                                           // 2^e_max * 1.mmm * 2^shared_exp over its element
     const uint32_t pos = b.index & 31u;
     const uint32_t lo = pos & 8u ? b.code[1] : b.code[0], hi = pos & 8u ? b.code[3] : b.code[2];
     const uint32_t nib = ((pos & 16u ? hi : lo) >> (4u * (pos & 7u))) & 15u;
     const uint32_t h = (((nib & 8u) << 12) | ((b.scale + 2u) << 7) | ((nib & 7u) << 4)) & keep;   // (scale byte 255: any number among NaN)
-    reinterpret_cast<u16a*>(dst)[pos] = (uint16_t)h;
+    *reinterpret_cast<u16a*>(tile + (at ^ (2u * pos))) = (uint16_t)h;
   }
 }
 
-// four tokens (rows `pitch` bytes apart) x 16 channels per 16 lanes, transposed: a lane gets four tokens of one channel
+// four tokens x 16 channels per 16 lanes, transposed: a lane gets four tokens of one channel
 __device__ __forceinline__ s16x4 read_transposed(const uint8_t* p) {
   return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)p);
 }
@@ -313,11 +333,13 @@ struct Walk {
   int part = -1;                                             // where a run's result goes: out, or among the parts
   __device__ __forceinline__ Walk(const AttnArgs& a, int rows, int unit, int least, Share& share, int64_t (&wave_sum)[kWaves]) {
     if (a.direct) {
-      uint32_t id = blockIdx.x;                              // tile of rows fastest, then key-value head, then sequence
-      tile = (int)(id % (uint32_t)a.row_tiles);
-      id /= (uint32_t)a.row_tiles;
+      // key-value head fastest (consecutive workgroups go to different XCDs: with 8 heads an XCD's cache has one to hold), then tile
+      // of rows, the longest first, then sequence
+      uint32_t id = blockIdx.x;
       kv_head = (int)(id % (uint32_t)a.g.kv_heads);
-      seq = (int)(id / (uint32_t)a.g.kv_heads);
+      id /= (uint32_t)a.g.kv_heads;
+      tile = (int)(id % (uint32_t)a.row_tiles);
+      seq = (int)(id / (uint32_t)a.row_tiles);
     } else {
       find_share(a, rows, unit, least, share, wave_sum);
       if (threadIdx.x == 0) a.joins[4 * blockIdx.x] = -1;
@@ -480,9 +502,7 @@ __device__ __forceinline__ void join_row_by_wave(const AttnArgs& a, int parts, P
 constexpr int kFewUnit = 32 * kWaves, kFewLeast = 4;          // tokens (a 32-token tile per wavefront); units per workgroup at least
 constexpr int kFewAhead = 1;                   // tiles in flight per wavefront
 template <int D>
-constexpr int few_pitch() { return 2 * D + 16; }             // bytes per token: 16 rows' 16-byte reads fall on all banks
-template <int D>
-constexpr int few_patch(int nt) { return 32 * few_pitch<D>() > 16 * nt * D * 4 ? 32 * few_pitch<D>() : 16 * nt * D * 4; }
+constexpr int few_patch(int nt) { return 64 * D * nt; }      // a tile of 32 tokens (2 D bytes each); 16 nt rows of fp32 for the join
 template <int D>
 constexpr int few_lds(int nt) { return kWaves * (few_patch<D>(nt) + 16 * nt * 8); }
 constexpr int few_waves_per_simd(int D, int NT) { return D * NT <= 128 ? 4 : D * NT <= 256 ? 2 : 1; }
@@ -490,9 +510,9 @@ constexpr int few_waves_per_simd(int D, int NT) { return D * NT <= 128 ? 4 : D *
 // NT tiles of 16 rows; TERMS: bf16 terms of P
 template <int D, int MODE, int NT, int TERMS>
 __global__ void __launch_bounds__(64 * kWaves, few_waves_per_simd(D, NT)) attn_few_kernel(const AttnArgs a) {
-  constexpr int DB = D / 32, NB = D / 64, PITCH = few_pitch<D>(), PATCH = few_patch<D>(NT);   // blocks per token; per lane of a 32-token tile
+  constexpr int DB = D / 32, NB = D / 64, PATCH = few_patch<D>(NT);   // blocks per token; per lane of a 32-token tile
   constexpr int LANE_TOKENS = D == 64 ? 32 : 16;             // tokens that a wavefront's lanes cover with one block each (of 2, 4, 4 neighbours)
-  extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
+  extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 15, quarter = lane >> 4;
   uint8_t* const patch = lds + wave * PATCH;                 // a tile's keys, then its values
@@ -571,9 +591,10 @@ __global__ void __launch_bounds__(64 * kWaves, few_waves_per_simd(D, NT)) attn_f
       uint64_t nan[NB];                                      // lanes whose block of V is NaN: zeros here, put in behind the product
       uint64_t any = 0;
 #pragma unroll
-      for (int i = 0; i < NB; ++i) expand<MODE>(f.k[i], false, patch + token_of(i) * PITCH + block_of(i) * 64);
+      for (int i = 0; i < NB; ++i) expand<MODE>(f.k[i], false, patch, formed_at_use(token_at<D>(token_of(i)) ^ (64u * block_of(i))));
       __builtin_amdgcn_wave_barrier();
       f32x4 sc[NT][2];
+      const uint32_t k_at = formed_at_use(token_at<D>(col) ^ (16u * quarter));
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
 #pragma unroll
@@ -581,7 +602,7 @@ __global__ void __launch_bounds__(64 * kWaves, few_waves_per_simd(D, NT)) attn_f
 #pragma unroll
         for (int st = 0; st < DB; ++st) {
           Operand k;
-          const u32x4 x = *reinterpret_cast<const u32x4*>(patch + (16 * h + col) * PITCH + (32 * st + 8 * quarter) * 2);
+          const u32x4 x = *reinterpret_cast<const u32x4*>(patch + 32 * D * h + (k_at ^ (64u * st)));
 #pragma unroll
           for (int j = 0; j < 4; ++j) k.u[j] = x[j];
 #pragma unroll
@@ -595,7 +616,7 @@ __global__ void __launch_bounds__(64 * kWaves, few_waves_per_simd(D, NT)) attn_f
         const bool dead = t0 + token >= span.end || !(token >= 16 ? h1 : h0);
         nan[i] = __ballot(f.v[i].scale == 255u && !dead);
         any |= nan[i];
-        expand<MODE>(f.v[i], dead || f.v[i].scale == 255u, patch + token * PITCH + block_of(i) * 64);
+        expand<MODE>(f.v[i], dead || f.v[i].scale == 255u, patch, formed_at_use(token_at<D>(token) ^ (64u * block_of(i))));
       }
       __builtin_amdgcn_wave_barrier();
       fetch(f, t0 + kFewAhead * 32 * kWaves);
@@ -626,12 +647,13 @@ __global__ void __launch_bounds__(64 * kWaves, few_waves_per_simd(D, NT)) attn_f
         }
         l[t] += weights<TERMS>(sc[t][0], sc[t][1], a.scale, base, p[t]);
       }
+      const uint32_t v_at = formed_at_use(token_at<D>(4 * quarter + (col >> 2)) ^ (8u * (col & 3)));
 #pragma unroll
       for (int d = 0; d < D / 16; ++d) {
         Operand v;
-        const uint8_t* at = patch + (4 * quarter + (col >> 2)) * PITCH + (16 * d + 4 * (col & 3)) * 2;
+        const uint8_t* at = patch + (v_at ^ (32u * d));
         v.s[0] = read_transposed(at);
-        v.s[1] = read_transposed(at + 16 * PITCH);
+        v.s[1] = read_transposed(at + 32 * D);
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -724,22 +746,22 @@ __global__ void __launch_bounds__(256) attn_join_kernel(const AttnArgs a, int ro
 // ---- many rows ------------------------------------------------------------------------------------------------------
 constexpr int kManyTokens = 64, kManyRows = 32 * kWaves, kManyLeast = 8;   // (a unit is a tile of tokens)
 template <int D>
-constexpr int many_pitch() { return 2 * D + 16; }
+constexpr int many_jobs() { return 2 * kManyTokens * (D / 32) / (64 * kWaves); }   // blocks of a tile per lane
 template <int D>
-constexpr int many_buffers() { return D == 256 ? 1 : 2; }    // (two of D = 256 exceed the 160 KiB of a compute unit together with nothing else)
-template <int D>
-constexpr int many_lds() { return many_buffers<D>() * 2 * kManyTokens * many_pitch<D>() + 2 * kWaves * 2 * 4 * 8; }
+constexpr int many_lds() { return 2 * 2 * kManyTokens * 2 * D + 2 * kWaves * many_jobs<D>() * 8; }   // two buffers of keys and values; NaN masks
 
 template <int D, int MODE, int TERMS>
 __global__ void __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) attn_many_kernel(const AttnArgs a) {
-  constexpr int DB = D / 32, NB = kManyTokens * DB / (64 * kWaves), PITCH = many_pitch<D>();
-  constexpr int BUF = many_buffers<D>(), HALF = kManyTokens * PITCH;
-  static_assert(NB * 64 * kWaves == kManyTokens * DB || D == 64, "blocks per lane");
-  constexpr int NL = NB < 1 ? 1 : NB;                        // D = 64: 128 blocks, the upper wavefronts have none
-  extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
-  uint64_t* const nans = reinterpret_cast<uint64_t*>(lds + BUF * 2 * HALF);   // [buffer][wave][NL] lanes with a NaN block of V
+  constexpr int DB = D / 32, HALF = kManyTokens * 2 * D, JOBS = many_jobs<D>();
+  extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
+  uint64_t* const nans = reinterpret_cast<uint64_t*>(lds + 4 * HALF);   // [buffer][wave][job] lanes with a NaN block of V
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 31, half = lane >> 5;
+  // The blocks of a tile that wavefront w expands, D >= 128: tokens 16 w ... + 15, keys in even jobs, values in odd ones, four blocks of a
+  // token per job; D = 64: tokens 32 (w % 2) ... + 31, keys for w < 2, values for the others
+  const auto job_of_v = [&](int k) { return D == 64 ? wave >> 1 : k & 1; };
+  const auto job_token = [&](int w, int who) { return D == 64 ? 32 * (w & 1) + (who & 31) : 16 * w + (who & 15); };
+  const auto job_block = [&](int k, int who) { return D == 64 ? who >> 5 : 4 * (k >> 1) + (who >> 4); };
   __shared__ Share share;
   __shared__ int64_t wave_sum[kWaves];
   for (Walk walk(a, kManyRows, kManyTokens, kManyLeast, share, wave_sum);;) {
@@ -775,49 +797,39 @@ __global__ void __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) attn_many_kerne
     for (int d = 0; d < DB; ++d)
 #pragma unroll
       for (int j = 0; j < 16; ++j) o[d][j] = 0.0f;
-    Block kb[NL], vb[NL];
+    Block job[JOBS];
     uint32_t held = 0, held_next = 0;                        // bit j: tokens 16 j ... + 15 of the tile have a page
     int fetched = 0;                                         // tiles
     int32_t pages = -1;                                      // lane n: the page of tokens 16 (n % 4) ... of tile n / 4 of the next 16
     const auto fetch = [&](int t) {
       if ((fetched & 15) == 0) pages = page_of(a, s, (int64_t)t + 16 * lane);
       held_next = 0;
-      const uint8_t* rec[4];
-      int at[4];
+      int32_t number[4];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const Page p(a, kv_head, __builtin_amdgcn_readlane(pages, 4 * (fetched & 15) + j), t + 16 * j);
-        held_next |= (p.held ? 1u : 0u) << j;
-        rec[j] = p.rec;
-        at[j] = p.at;
+        number[j] = __builtin_amdgcn_readlane(pages, 4 * (fetched & 15) + j);
+        held_next |= (number[j] >= 0 ? 1u : 0u) << j;
       }
       ++fetched;
+      // this wavefront's tokens lie in one 16-token group of the tile (D = 64: in two)
+      const int group = D == 64 ? 2 * (wave & 1) : wave;
+      const int32_t n0 = D == 64 ? (wave & 1 ? number[2] : number[0]) : wave & 2 ? (wave & 1 ? number[3] : number[2]) : (wave & 1 ? number[1] : number[0]);
+      const Page p0(a, kv_head, n0, t + 16 * group), p1(a, kv_head, D == 64 ? (wave & 1 ? number[3] : number[1]) : n0, t + 16 * group + 16);
+      const bool second = D == 64 && (lane & 16);
+      const uint8_t* const rec = second ? p1.rec : p0.rec;
+      const int row = (second ? p1.at : p0.at) + (lane & 15);
 #pragma unroll
-      for (int k = 0; k < NL; ++k) {
-        const int n = (int)threadIdx.x + 64 * kWaves * k, token = n / DB;
-        if (token < kManyTokens) {
-          const int j = token >> 4;
-          const uint8_t* base = j & 2 ? (j & 1 ? rec[3] : rec[2]) : (j & 1 ? rec[1] : rec[0]);
-          const int row = (j & 2 ? (j & 1 ? at[3] : at[2]) : (j & 1 ? at[1] : at[0])) + (token & 15);
-          kb[k] = load_block<D, MODE>(base, a.g, row, n % DB);
-          vb[k] = load_block<D, MODE>(base + a.g.part_bytes, a.g, row, n % DB);
-        }
-      }
+      for (int k = 0; k < JOBS; ++k) job[k] = load_block<D, MODE>(rec + (job_of_v(k) ? a.g.part_bytes : 0), a.g, row, job_block(k, lane));
     };
     const auto expand_all = [&](int t, int buf) {            // the fetched tile into a buffer
-      uint8_t* const kt = lds + buf * 2 * HALF;
+      const int token = job_token(wave, lane);
+      const bool dead = t + token >= span.end || !((held_next >> (token >> 4)) & 1u);
 #pragma unroll
-      for (int k = 0; k < NL; ++k) {
-        const int n = (int)threadIdx.x + 64 * kWaves * k, token = n / DB;
-        bool bad = false;
-        if (token < kManyTokens) {
-          const bool dead = t + token >= span.end || !((held_next >> (token >> 4)) & 1u);
-          expand<MODE>(kb[k], false, kt + token * PITCH + (n % DB) * 64);
-          bad = vb[k].scale == 255u && !dead;
-          expand<MODE>(vb[k], dead || bad, kt + HALF + token * PITCH + (n % DB) * 64);
-        }
-        const uint64_t b = __ballot(bad);
-        if (lane == 0) nans[(buf * kWaves + wave) * NL + k] = b;
+      for (int k = 0; k < JOBS; ++k) {
+        const bool nan = job_of_v(k) && job[k].scale == 255u;
+        expand<MODE>(job[k], job_of_v(k) && (dead || nan), lds + buf * 2 * HALF + job_of_v(k) * HALF, token_at<D>(token) ^ (64u * job_block(k, lane)));
+        const uint64_t b = __ballot(nan && !dead);
+        if (lane == 0) nans[(buf * kWaves + wave) * JOBS + k] = b;
       }
     };
     int buf = 0;
@@ -841,7 +853,7 @@ __global__ void __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) attn_many_kerne
 #pragma unroll
           for (int st = 0; st < D / 16; ++st) {
             Operand k;
-            const u32x4 x = *reinterpret_cast<const u32x4*>(kt + (32 * h + col) * PITCH + (16 * st + 8 * half) * 2);
+            const u32x4 x = *reinterpret_cast<const u32x4*>(kt + 64 * D * h + (token_at<D>(col) ^ (16u * half) ^ (32u * st)));
 #pragma unroll
             for (int j = 0; j < 4; ++j) k.u[j] = x[j];
             sc[h] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k.v, q[st].v, sc[h], 0, 0, 0);
@@ -880,33 +892,31 @@ __global__ void __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) attn_many_kerne
 #pragma unroll
           for (int d = 0; d < DB; ++d) {
             Operand v;
-            const uint8_t* at = vt + (16 * b + 4 * half + ((lane & 15) >> 2)) * PITCH + (32 * d + 16 * ((lane >> 4) & 1) + 4 * (lane & 3)) * 2;
-            v.s[0] = read_transposed(at);
-            v.s[1] = read_transposed(at + 8 * PITCH);
+            const uint32_t at = token_at<D>(4 * half + ((lane & 15) >> 2)) ^ (32u * ((lane >> 4) & 1)) ^ (8u * (lane & 3)) ^ (64u * d);
+            v.s[0] = read_transposed(vt + 32 * D * b + at);
+            v.s[1] = read_transposed(vt + 32 * D * b + 16 * D + (at ^ 32u));   // eight tokens on: s differs in bit 1
 #pragma unroll
             for (int c = 0; c < TERMS; ++c) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v.v, p[c].v, o[d], 0, 0, 0);
           }
         }
         uint64_t any = 0;
 #pragma unroll
-        for (int k = 0; k < kWaves * NL; ++k) any |= nans[buf * kWaves * NL + k];
+        for (int k = 0; k < kWaves * JOBS; ++k) any |= nans[buf * kWaves * JOBS + k];
         if (__any(any != 0)) {                               // NaN blocks of V, for the rows that see them
-          for (int k = 0; k < kWaves * NL; ++k)
-            for (uint64_t left = nans[buf * kWaves * NL + k]; left; left &= left - 1) {
-              const int n = __builtin_ctzll(left) + 64 * (k / NL) + 64 * kWaves * (k % NL), tok = t0 + n / DB;
-              if (tok >= first && tok <= last) {
+#pragma unroll 1
+          for (int k = 0; k < kWaves * JOBS; ++k)
+            for (uint64_t left = nans[buf * kWaves * JOBS + k]; left; left &= left - 1) {
+              const int who = __builtin_ctzll(left), tok = t0 + job_token(k / JOBS, who), blk = job_block(k % JOBS, who);
+              const bool seen = tok >= first && tok <= last;
 #pragma unroll
-                for (int d = 0; d < DB; ++d)
-                  if (d == n % DB)
+              for (int d = 0; d < DB; ++d)
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) o[d][j] = __uint_as_float(0x7FC00000u);
-              }
+                for (int j = 0; j < 16; ++j) o[d][j] = seen && d == blk ? __uint_as_float(0x7FC00000u) : o[d][j];
             }
         }
       }
       if (more) {
-        if (BUF == 1) __syncthreads();                       // everyone is done with the only buffer
-        else buf ^= 1;
+        buf ^= 1;
         expand_all(t0 + kManyTokens, buf);
       }
     }
