@@ -172,11 +172,13 @@ struct Block {
   uint32_t scale, index;
 };
 
-template <int D, int MODE>
+// ONCE: no other workgroup of the call reads these codes (64 sequences of 2048 to 8192 tokens 98.6 -> 93.5 us with streaming loads)
+template <int D, int MODE, bool ONCE>
 __device__ __forceinline__ Block load_block(const uint8_t* rec, const CacheGeom& g, int row, int blk) {
   Block b;
   const int n = row * (D / 32) + blk;
-  b.code = *reinterpret_cast<const u32x4*>(rec + n * 16);
+  const u32x4* const code = reinterpret_cast<const u32x4*>(rec + n * 16);
+  b.code = ONCE ? __builtin_nontemporal_load(code) : *code;
   b.scale = rec[g.scales_at + n];
   b.index = MODE >= 1 ? rec[g.index_at + n] : 0u;
   return b;
@@ -504,19 +506,22 @@ constexpr int kFewAhead = 1;                   // tiles in flight per wavefront
 template <int D>
 constexpr int few_patch(int nt) { return 64 * D * nt; }      // a tile of 32 tokens (2 D bytes each); 16 nt rows of fp32 for the join
 template <int D>
-constexpr int few_lds(int nt) { return kWaves * (few_patch<D>(nt) + 16 * nt * 8); }
+constexpr int few_lds(int nt, int waves) { return waves * (few_patch<D>(nt) + 16 * nt * 8); }
+// Wavefronts of a workgroup that has a compute unit to itself, as many as LDS and registers hold: where there are few rows and heads
+// in all, a tile of tokens takes 1.6 us, whatever runs beside it (one sequence of 512 tokens 13.1 us with 4, 9.0 with 16).
+constexpr int few_waves_alone(int D, int NT) { return D * NT <= 128 ? 16 : D * NT <= 256 ? 8 : 4; }
 constexpr int few_waves_per_simd(int D, int NT) { return D * NT <= 128 ? 4 : D * NT <= 256 ? 2 : 1; }
 
 // NT tiles of 16 rows; TERMS: bf16 terms of P
-template <int D, int MODE, int NT, int TERMS>
-__global__ void __launch_bounds__(64 * kWaves, few_waves_per_simd(D, NT)) attn_few_kernel(const AttnArgs a) {
+template <int D, int MODE, int NT, int TERMS, int WAVES>
+__global__ void __launch_bounds__(64 * WAVES, few_waves_per_simd(D, NT)) attn_few_kernel(const AttnArgs a) {
   constexpr int DB = D / 32, NB = D / 64, PATCH = few_patch<D>(NT);   // blocks per token; per lane of a 32-token tile
   constexpr int LANE_TOKENS = D == 64 ? 32 : 16;             // tokens that a wavefront's lanes cover with one block each (of 2, 4, 4 neighbours)
   extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 15, quarter = lane >> 4;
   uint8_t* const patch = lds + wave * PATCH;                 // a tile's keys, then its values
-  float* const ml = reinterpret_cast<float*>(lds + kWaves * PATCH);   // [wave][row][2]
+  float* const ml = reinterpret_cast<float*>(lds + WAVES * PATCH);   // [wave][row][2]
   // this lane's blocks of a tile: its token (16 lanes in a row have 16 tokens: their stores fall on all banks), its block of the token
   const auto token_of = [&](int i) { return D == 256 ? 16 * (i >> 1) + (lane & 15) : LANE_TOKENS * i + (lane & (LANE_TOKENS - 1)); };
   const auto block_of = [&](int i) { return D == 256 ? 4 * (i & 1) + (lane >> 4) : lane / LANE_TOKENS; };
@@ -559,7 +564,7 @@ __global__ void __launch_bounds__(64 * kWaves, few_waves_per_simd(D, NT)) attn_f
 #pragma unroll
       for (int d = 0; d < D / 16; ++d) o[t][d] = f32x4{0, 0, 0, 0};
     }
-    // The wavefront's tiles: span.begin + 32 wave, and every 32 kWaves tokens from there.  Lane n holds the page of half n % 2 of
+    // The wavefront's tiles: span.begin + 32 wave, and every 32 WAVES tokens from there.  Lane n holds the page of half n % 2 of
     // tile n / 2 of the next 32 tiles (-1: none), so that a tile's addresses wait for no table.
     const int begin = span.begin + 32 * wave;
     int fetched = 0;                                         // tiles
@@ -570,7 +575,7 @@ __global__ void __launch_bounds__(64 * kWaves, few_waves_per_simd(D, NT)) attn_f
     } ahead[kFewAhead];
     const auto fetch = [&](Fetched& f, int t) {
       if (t >= span.end) return;
-      if ((fetched & 31) == 0) pages = page_of(a, s, (int64_t)t + 32 * kWaves * (lane >> 1) + 16 * (lane & 1));
+      if ((fetched & 31) == 0) pages = page_of(a, s, (int64_t)t + 32 * WAVES * (lane >> 1) + 16 * (lane & 1));
       const Page p0(a, kv_head, __builtin_amdgcn_readlane(pages, 2 * (fetched & 31)), t), p1(a, kv_head, __builtin_amdgcn_readlane(pages, 2 * (fetched & 31) + 1), t + 16);
       f.held0 = p0.held;
       f.held1 = p1.held;
@@ -581,8 +586,8 @@ __global__ void __launch_bounds__(64 * kWaves, few_waves_per_simd(D, NT)) attn_f
         const bool second = D == 64 ? token >= 16 : i >= NB / 2;
         const uint8_t* rec = second ? p1.rec : p0.rec;
         const int row = second ? p1.at + (token & 15) : p0.at + token;
-        f.k[i] = load_block<D, MODE>(rec, a.g, row, block_of(i));
-        f.v[i] = load_block<D, MODE>(rec + a.g.part_bytes, a.g, row, block_of(i));
+        f.k[i] = load_block<D, MODE, true>(rec, a.g, row, block_of(i));
+        f.v[i] = load_block<D, MODE, true>(rec + a.g.part_bytes, a.g, row, block_of(i));
       }
     };
     const auto take = [&](Fetched& f, int t0) {
@@ -619,7 +624,7 @@ __global__ void __launch_bounds__(64 * kWaves, few_waves_per_simd(D, NT)) attn_f
         expand<MODE>(f.v[i], dead || f.v[i].scale == 255u, patch, formed_at_use(token_at<D>(token) ^ (64u * block_of(i))));
       }
       __builtin_amdgcn_wave_barrier();
-      fetch(f, t0 + kFewAhead * 32 * kWaves);
+      fetch(f, t0 + kFewAhead * 32 * WAVES);
       const bool whole = h0 && h1 && t0 >= all_from && t0 + 31 <= all_to && t0 + 32 <= span.end;   // (uniform)
       if (!whole) {
 #pragma unroll
@@ -681,10 +686,10 @@ __global__ void __launch_bounds__(64 * kWaves, few_waves_per_simd(D, NT)) attn_f
       __builtin_amdgcn_wave_barrier();
     };
 #pragma unroll
-    for (int u = 0; u < kFewAhead; ++u) fetch(ahead[u], begin + u * 32 * kWaves);
-    for (int t0 = begin; t0 < span.end; t0 += kFewAhead * 32 * kWaves)
+    for (int u = 0; u < kFewAhead; ++u) fetch(ahead[u], begin + u * 32 * WAVES);
+    for (int t0 = begin; t0 < span.end; t0 += kFewAhead * 32 * WAVES)
 #pragma unroll
-      for (int u = 0; u < kFewAhead; ++u) take(ahead[u], t0 + u * 32 * kWaves);
+      for (int u = 0; u < kFewAhead; ++u) take(ahead[u], t0 + u * 32 * WAVES);
     // join the wavefronts: each leaves its rows in its own patch
     float* const mine = reinterpret_cast<float*>(patch);
 #pragma unroll
@@ -698,16 +703,16 @@ __global__ void __launch_bounds__(64 * kWaves, few_waves_per_simd(D, NT)) attn_f
       for (int d = 0; d < D / 16; ++d) *reinterpret_cast<f32x4*>(mine + (16 * t + col) * D + 16 * d + 4 * quarter) = o[t][d];
     }
     __syncthreads();
-    for (int j = threadIdx.x; j < 16 * NT * (D / 4); j += 64 * kWaves) {
+    for (int j = threadIdx.x; j < 16 * NT * (D / 4); j += 64 * WAVES) {
       const int row = j / (D / 4), d = (j - row * (D / 4)) * 4, r = r0 + row;
       if (r >= R) break;
       float top = -kInf, sum = 0.0f;
 #pragma unroll
-      for (int v = 0; v < kWaves; ++v) top = fmaxf(top, ml[(v * 16 * NT + row) * 2]);
+      for (int v = 0; v < WAVES; ++v) top = fmaxf(top, ml[(v * 16 * NT + row) * 2]);
       const float base = zero_if_none(top);
       f32x4 out = {0, 0, 0, 0};
 #pragma unroll
-      for (int v = 0; v < kWaves; ++v) {
+      for (int v = 0; v < WAVES; ++v) {
         const float f = exp2_of(ml[(v * 16 * NT + row) * 2] - base);
         sum += ml[(v * 16 * NT + row) * 2 + 1] * f;
         out += *reinterpret_cast<const f32x4*>(lds + v * PATCH + (row * D + d) * 4) * f;
@@ -819,7 +824,7 @@ __global__ void __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) attn_many_kerne
       const uint8_t* const rec = second ? p1.rec : p0.rec;
       const int row = (second ? p1.at : p0.at) + (lane & 15);
 #pragma unroll
-      for (int k = 0; k < JOBS; ++k) job[k] = load_block<D, MODE>(rec + (job_of_v(k) ? a.g.part_bytes : 0), a.g, row, job_block(k, lane));
+      for (int k = 0; k < JOBS; ++k) job[k] = load_block<D, MODE, false>(rec + (job_of_v(k) ? a.g.part_bytes : 0), a.g, row, job_block(k, lane));
     };
     const auto expand_all = [&](int t, int buf) {            // the fetched tile into a buffer
       const int token = job_token(wave, lane);
@@ -936,7 +941,7 @@ __global__ void __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) attn_many_kerne
 
 // ---- launch -----------------------------------------------------------------------------------------------------------
 struct Plan {
-  bool many, direct;
+  bool many, direct, alone;                                  // alone: a workgroup per compute unit at most
   int rows, row_tiles;                                       // of a tile, tiles per key-value head and sequence
   int64_t wgs;
 };
@@ -961,6 +966,7 @@ Plan plan_for(int64_t n_seq, int64_t max_q, int64_t max_kv, int64_t heads, int64
   const int64_t unit = p.many ? kManyTokens : kFewUnit, least = p.many ? kManyLeast : kFewLeast, units = items * ((len + unit - 1) / unit);
   const bool prompt = p.many && causal && 2 * max_q > len && 2 * items > room;
   p.direct = len <= (p.many ? kManyDirect : kFewDirect) || items >= 4 * room || prompt;
+  p.alone = !p.many && p.direct && items <= kNumCU;
   p.wgs = p.direct ? items : units < least * room ? (units + least - 1) / least : room;
   return p;
 }
@@ -969,6 +975,18 @@ Plan plan_for(int64_t n_seq, int64_t max_q, int64_t max_kv, int64_t heads, int64
 int64_t part_rows(const Plan& p) { return p.direct ? 0 : p.wgs * 2 * p.rows; }
 size_t parts_bytes(const Plan& p, int64_t D) { return p.direct ? 0 : (size_t)part_rows(p) * (size_t)(D + 2) * 4 + (size_t)p.wgs * 16; }
 
+template <int D, int MODE, int NT, int TERMS, int WAVES>
+void launch_few(const AttnArgs& a, const Plan& p, hipStream_t s) {
+  constexpr int bytes = few_lds<D>(NT, WAVES);
+  allow_dynamic_lds<attn_few_kernel<D, MODE, NT, TERMS, WAVES>>(bytes);
+  hipLaunchKernelGGL((attn_few_kernel<D, MODE, NT, TERMS, WAVES>), dim3((unsigned)p.wgs), dim3(64 * WAVES), bytes, s, a);
+}
+template <int D, int MODE, int NT, int TERMS>
+void launch_few(const AttnArgs& a, const Plan& p, hipStream_t s) {
+  if (p.alone) launch_few<D, MODE, NT, TERMS, few_waves_alone(D, NT)>(a, p, s);
+  else launch_few<D, MODE, NT, TERMS, kWaves>(a, p, s);
+}
+
 template <int D, int MODE, int TERMS>
 void launch(const AttnArgs& a, const Plan& p, hipStream_t s) {
   const dim3 grid((unsigned)p.wgs);
@@ -976,11 +994,9 @@ void launch(const AttnArgs& a, const Plan& p, hipStream_t s) {
     allow_dynamic_lds<attn_many_kernel<D, MODE, TERMS>>(many_lds<D>());
     hipLaunchKernelGGL((attn_many_kernel<D, MODE, TERMS>), grid, dim3(64 * kWaves), many_lds<D>(), s, a);
   } else if (p.rows == 32) {
-    allow_dynamic_lds<attn_few_kernel<D, MODE, 2, TERMS>>(few_lds<D>(2));
-    hipLaunchKernelGGL((attn_few_kernel<D, MODE, 2, TERMS>), grid, dim3(64 * kWaves), few_lds<D>(2), s, a);
+    launch_few<D, MODE, 2, TERMS>(a, p, s);
   } else {
-    allow_dynamic_lds<attn_few_kernel<D, MODE, 1, TERMS>>(few_lds<D>(1));
-    hipLaunchKernelGGL((attn_few_kernel<D, MODE, 1, TERMS>), grid, dim3(64 * kWaves), few_lds<D>(1), s, a);
+    launch_few<D, MODE, 1, TERMS>(a, p, s);
   }
 }
 
