@@ -48,61 +48,86 @@ struct Place {
   }
 };
 
-template <bool BF16, int MODE>
+// Groups per lane, U: kCacheUnroll with their loads under way together where there are rows enough for the whole chip
+// (see cache_unroll), else one.
+template <bool BF16, int MODE, int U>
 __global__ void __launch_bounds__(256) cache_quantize_kernel(const CacheRows a, int64_t n_wg) {
   const int part = threadIdx.x & 3;
-  for (int64_t wg = blockIdx.x; wg < n_wg; wg += gridDim.x) {
-    Place p;
-    const bool there = p.find(a, wg) && p.held(a);
-    uint32_t w[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    if (there) {
-      const void* src = p.is_v ? a.v : a.k;
-      if (BF16) {
-        const u32x4 t = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(src) + p.value(a));
-        w[0] = t.x; w[1] = t.y; w[2] = t.z; w[3] = t.w;
-      } else {
-        const u32x4* q = reinterpret_cast<const u32x4*>(static_cast<const float*>(src) + p.value(a));
-        const u32x4 t0 = q[0], t1 = q[1];
-        w[0] = t0.x; w[1] = t0.y; w[2] = t0.z; w[3] = t0.w;
-        w[4] = t1.x; w[5] = t1.y; w[6] = t1.z; w[7] = t1.w;
+  for (int64_t wg = (int64_t)blockIdx.x * U; wg < n_wg; wg += (int64_t)gridDim.x * U) {
+    Place p[U];
+    bool there[U];
+    uint32_t w[U][8];
+#pragma unroll
+    for (int u = 0; u < U; ++u) there[u] = p[u].find(a, wg + u);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      there[u] = there[u] && p[u].held(a);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) w[u][i] = 0;
+      if (there[u]) {
+        const void* src = p[u].is_v ? a.v : a.k;
+        if (BF16) {
+          const u32x4 t = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(src) + p[u].value(a)));
+          w[u][0] = t.x; w[u][1] = t.y; w[u][2] = t.z; w[u][3] = t.w;
+        } else {
+          const u32x4* q = reinterpret_cast<const u32x4*>(static_cast<const float*>(src) + p[u].value(a));
+          const u32x4 t0 = __builtin_nontemporal_load(q), t1 = __builtin_nontemporal_load(q + 1);
+          w[u][0] = t0.x; w[u][1] = t0.y; w[u][2] = t0.z; w[u][3] = t0.w;
+          w[u][4] = t1.x; w[u][5] = t1.y; w[u][6] = t1.z; w[u][7] = t1.w;
+        }
       }
     }
-    uint32_t sbyte, idx;
-    const uint32_t packed = encode_group<BF16, MODE>(w, part, sbyte, idx);   // (every lane: the quad exchanges)
-    if (there) {
-      uint8_t* rec = p.record(a);
-      const int row = p.row(a);
-      *reinterpret_cast<uint32_t*>(rec + row * (a.g.D >> 1) + p.group * 4) = packed;
-      if (part == 0) {
-        const int b = row * (a.g.D >> 5) + (p.group >> 2);
-        rec[a.g.scales_at + b] = (uint8_t)sbyte;
-        if (MODE >= 1) rec[a.g.index_at + b] = (uint8_t)idx;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      uint32_t sbyte, idx;
+      const uint32_t packed = encode_group<BF16, MODE>(w[u], part, sbyte, idx);   // (every lane: the quad exchanges)
+      if (there[u]) {
+        uint8_t* rec = p[u].record(a);
+        const int row = p[u].row(a);
+        *reinterpret_cast<uint32_t*>(rec + row * (a.g.D >> 1) + p[u].group * 4) = packed;
+        if (part == 0) {
+          const int b = row * (a.g.D >> 5) + (p[u].group >> 2);
+          rec[a.g.scales_at + b] = (uint8_t)sbyte;
+          if (MODE >= 1) rec[a.g.index_at + b] = (uint8_t)idx;
+        }
       }
     }
   }
 }
 
-template <bool BF16, int MODE>
+template <bool BF16, int MODE, int U>
 __global__ void __launch_bounds__(256) cache_dequantize_kernel(const CacheRows a, void* k, void* v, int64_t n_wg) {
   const uint32_t part = threadIdx.x & 3u;
-  for (int64_t wg = blockIdx.x; wg < n_wg; wg += gridDim.x) {
-    Place p;
-    if (!p.find(a, wg)) continue;
-    uint32_t out[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    if (p.held(a)) {
-      const uint8_t* rec = p.record(a);
-      const int row = p.row(a), b = row * (a.g.D >> 5) + (p.group >> 2);
-      const uint32_t dw = *reinterpret_cast<const uint32_t*>(rec + row * (a.g.D >> 1) + p.group * 4);
-      const uint32_t sbyte = rec[a.g.scales_at + b], ib = MODE >= 1 ? rec[a.g.index_at + b] : 0u;
-      decode_group<(MODE >= 1), BF16>(dw, sbyte, MODE >= 1 ? ib & 31u : 64u, part, out, MODE == 2 ? ib >> 5 : 0u);
+  for (int64_t wg = (int64_t)blockIdx.x * U; wg < n_wg; wg += (int64_t)gridDim.x * U) {
+    Place p[U];
+    bool there[U];
+    uint32_t dw[U], sbyte[U], ib[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) there[u] = p[u].find(a, wg + u);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      dw[u] = sbyte[u] = ib[u] = 0;                          // (scale byte 0: zeros)
+      if (there[u] && p[u].held(a)) {
+        const uint8_t* rec = p[u].record(a);
+        const int row = p[u].row(a), b = row * (a.g.D >> 5) + (p[u].group >> 2);
+        dw[u] = *reinterpret_cast<const uint32_t*>(rec + row * (a.g.D >> 1) + p[u].group * 4);
+        sbyte[u] = rec[a.g.scales_at + b];
+        if (MODE >= 1) ib[u] = rec[a.g.index_at + b];
+      }
     }
-    void* dst = p.is_v ? v : k;
-    if (BF16) {
-      *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(dst) + p.value(a)) = u32x4{out[0], out[1], out[2], out[3]};
-    } else {
-      u32x4* o = reinterpret_cast<u32x4*>(static_cast<float*>(dst) + p.value(a));
-      o[0] = u32x4{out[0], out[1], out[2], out[3]};
-      o[1] = u32x4{out[4], out[5], out[6], out[7]};
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (!there[u]) continue;
+      uint32_t out[8];
+      decode_group<(MODE >= 1), BF16>(dw[u], sbyte[u], MODE >= 1 ? ib[u] & 31u : 64u, part, out, MODE == 2 ? ib[u] >> 5 : 0u);
+      void* dst = p[u].is_v ? v : k;
+      if (BF16) {
+        __builtin_nontemporal_store(u32x4{out[0], out[1], out[2], out[3]}, reinterpret_cast<u32x4*>(static_cast<uint16_t*>(dst) + p[u].value(a)));
+      } else {
+        u32x4* o = reinterpret_cast<u32x4*>(static_cast<float*>(dst) + p[u].value(a));
+        __builtin_nontemporal_store(u32x4{out[0], out[1], out[2], out[3]}, o);
+        __builtin_nontemporal_store(u32x4{out[4], out[5], out[6], out[7]}, o + 1);
+      }
     }
   }
 }
@@ -133,7 +158,12 @@ int check_rows(const void* k, const void* v, int dtype, int64_t tokens, int64_t 
   return MXP_OK;
 }
 
-unsigned grid_of(int64_t n_wg) { return (unsigned)(n_wg < ((int64_t)1 << 24) ? n_wg : ((int64_t)1 << 24)); }
+constexpr int kCacheUnroll = 4;
+bool cache_unroll(int64_t n_wg) { return n_wg >= (int64_t)kNumCU * 8 * kCacheUnroll; }   // a full chip of workgroups with four groups per lane
+unsigned grid_of(int64_t n_wg) {
+  const int64_t n = cache_unroll(n_wg) ? (n_wg + kCacheUnroll - 1) / kCacheUnroll : n_wg;
+  return (unsigned)(n < ((int64_t)1 << 24) ? n : ((int64_t)1 << 24));
+}
 
 }  // namespace
 
@@ -152,7 +182,11 @@ extern "C" int mxp_cache_write(const void* K, const void* V, int src_dtype, int6
   if (rc != MXP_OK || tokens == 0) return rc;
   const dim3 grid(grid_of(n_wg)), block(256);
   hipStream_t s = static_cast<hipStream_t>(stream);
-#define MXP_WRITE(B, M) hipLaunchKernelGGL((cache_quantize_kernel<B, M>), grid, block, 0, s, a, n_wg)
+#define MXP_WRITE(B, M)                                                                                            \
+  do {                                                                                                             \
+    if (cache_unroll(n_wg)) hipLaunchKernelGGL((cache_quantize_kernel<B, M, kCacheUnroll>), grid, block, 0, s, a, n_wg); \
+    else hipLaunchKernelGGL((cache_quantize_kernel<B, M, 1>), grid, block, 0, s, a, n_wg);                         \
+  } while (0)
   if (src_dtype == MXP_BF16) { if (fmt == 0) MXP_WRITE(true, 0); else if (fmt == 1) MXP_WRITE(true, 1); else MXP_WRITE(true, 2); }
   else                       { if (fmt == 0) MXP_WRITE(false, 0); else if (fmt == 1) MXP_WRITE(false, 1); else MXP_WRITE(false, 2); }
 #undef MXP_WRITE
@@ -168,7 +202,11 @@ extern "C" int mxp_cache_read(const void* cache, int64_t n_pages, int64_t page_t
   if (rc != MXP_OK || tokens == 0) return rc;
   const dim3 grid(grid_of(n_wg)), block(256);
   hipStream_t s = static_cast<hipStream_t>(stream);
-#define MXP_READ(B, M) hipLaunchKernelGGL((cache_dequantize_kernel<B, M>), grid, block, 0, s, a, K, V, n_wg)
+#define MXP_READ(B, M)                                                                                             \
+  do {                                                                                                             \
+    if (cache_unroll(n_wg)) hipLaunchKernelGGL((cache_dequantize_kernel<B, M, kCacheUnroll>), grid, block, 0, s, a, K, V, n_wg); \
+    else hipLaunchKernelGGL((cache_dequantize_kernel<B, M, 1>), grid, block, 0, s, a, K, V, n_wg);                 \
+  } while (0)
   if (dst_dtype == MXP_BF16) { if (fmt == 0) MXP_READ(true, 0); else if (fmt == 1) MXP_READ(true, 1); else MXP_READ(true, 2); }
   else                       { if (fmt == 0) MXP_READ(false, 0); else if (fmt == 1) MXP_READ(false, 1); else MXP_READ(false, 2); }
 #undef MXP_READ

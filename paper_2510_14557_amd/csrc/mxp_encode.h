@@ -7,6 +7,9 @@ namespace mxp {
 
 typedef __bf16 enc_v2bf __attribute__((ext_vector_type(2)));
 typedef short enc_v2s __attribute__((ext_vector_type(2)));
+typedef __bf16 enc_v32bf __attribute__((ext_vector_type(32)));
+typedef float enc_v16f __attribute__((ext_vector_type(16)));
+typedef uint32_t enc_v6u __attribute__((ext_vector_type(6)));
 
 template <int CTRL>
 __device__ __forceinline__ uint32_t dpp_mov(uint32_t v) {
@@ -266,6 +269,78 @@ __device__ __forceinline__ void encode_wide_group(const uint32_t (&raw)[8], cons
   idx = pos;
   if (flush || nonfinite) {
     lo = hi = 0;
+    idx = 0;
+    sb = nonfinite ? 255u : 0u;
+  }
+}
+
+// The same for MXFP6 / MXFP6+ through the 32-element pack-convert: every lane of the quad collects the whole block and converts it,
+// lanes 0..2 keep 8 of the 24 bytes each (s0, s1; lane 3's are no part of it).  w: as loaded, 4 dwords of bf16 pairs or 8 of fp32.
+constexpr int kQuadLane0 = 0x00, kQuadLane1 = 0x55, kQuadLane2 = 0xAA, kQuadLane3 = 0xFF;   // quad_perm broadcasts
+template <bool BF16, bool PLUS>
+__device__ __forceinline__ void encode_fp6_group(const uint32_t (&w)[BF16 ? 4 : 8], const uint32_t (&a)[8], uint32_t part, uint32_t& s0,
+                                                 uint32_t& s1, uint32_t& sb, uint32_t& idx) {
+  using F = Elem<6>;
+  constexpr int NW = BF16 ? 4 : 8;
+  uint32_t mx = a[0];
+#pragma unroll
+  for (int i = 1; i < 8; ++i) mx = umax(mx, a[i]);
+  mx = umax(mx, dpp_mov<kQuadSwap1>(mx));
+  mx = umax(mx, dpp_mov<kQuadSwap2>(mx));
+  uint32_t pos = 32u;                             // lowest position holding the maximum
+#pragma unroll
+  for (int i = 7; i >= 0; --i) pos = a[i] == mx ? part * 8u + (uint32_t)i : pos;
+  pos = umin(pos, dpp_mov<kQuadSwap1>(pos));
+  pos = umin(pos, dpp_mov<kQuadSwap2>(pos));
+  const uint32_t E = mx >> 23;
+  const bool flush = E <= (uint32_t)F::EMAX, nonfinite = E == 255u;
+  const int sbyte = (int)E - F::EMAX;
+  const float X = __uint_as_float((uint32_t)(sbyte > 0 ? sbyte : 1) << 23);
+  // the whole block in every lane of the quad
+  uint32_t all[4 * NW];
+#pragma unroll
+  for (int j = 0; j < NW; ++j) {
+    all[0 * NW + j] = dpp_mov<kQuadLane0>(w[j]);
+    all[1 * NW + j] = dpp_mov<kQuadLane1>(w[j]);
+    all[2 * NW + j] = dpp_mov<kQuadLane2>(w[j]);
+    all[3 * NW + j] = dpp_mov<kQuadLane3>(w[j]);
+  }
+  enc_v6u r;
+  if (BF16) {
+    union { uint32_t u[16]; enc_v32bf v; } c;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) c.u[i] = all[i];
+    r = __builtin_amdgcn_cvt_scalef32_pk32_fp6_bf16(c.v, X);
+  } else {
+    enc_v16f lo16, hi16;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {                   // the two sources are interleaved: code 2i from the first, 2i + 1 from the second
+      lo16[i] = __uint_as_float(all[2 * i]);
+      hi16[i] = __uint_as_float(all[2 * i + 1]);
+    }
+    r = __builtin_amdgcn_cvt_scalef32_2xpk16_fp6_f32(lo16, hi16, X);
+  }
+  // this lane's share: dwords 2 part, 2 part + 1 (lane 3 stores nothing)
+  s0 = part == 0u ? r[0] : (part == 1u ? r[2] : r[4]);
+  s1 = part == 0u ? r[1] : (part == 1u ? r[3] : r[5]);
+  if (PLUS) {
+    // the BM's magnitude mmmmm at bit 6 pos of the block's string = bit rel of this share (may hang over either edge); its
+    // sign is there already: a BM is at least 4 X, and the conversion keeps the sign
+    const uint32_t code = bm_code<6>(mx);
+    const int rel = (int)(6u * pos) - 64 * (int)part;
+    uint64_t share = ((uint64_t)s1 << 32) | s0;
+    if (rel > -6 && rel < 64) {
+      const uint64_t m = rel >= 0 ? ((uint64_t)0x1Fu << rel) : ((uint64_t)0x1Fu >> (-rel));
+      const uint64_t c = rel >= 0 ? ((uint64_t)code << rel) : ((uint64_t)code >> (-rel));
+      share = (share & ~m) | c;
+    }
+    s0 = (uint32_t)share;
+    s1 = (uint32_t)(share >> 32);
+  }
+  sb = (uint32_t)sbyte;
+  idx = pos;
+  if (flush || nonfinite) {
+    s0 = s1 = 0;
     idx = 0;
     sb = nonfinite ? 255u : 0u;
   }

@@ -82,25 +82,19 @@ __device__ __forceinline__ void convert_store(const NormArgs& a, int64_t row, in
     const uint32_t packed = encode_group<false, FMT>(raw, (int)part, sb, idx);
     reinterpret_cast<uint32_t*>(a.elems)[blk * 4 + part] = packed;
   } else {
-    constexpr int BITS = FMT <= MXP_FMT_MXFP6P ? 6 : 8;
+    constexpr bool PLUS = FMT == MXP_FMT_MXFP6P || FMT == MXP_FMT_MXFP8P;
     uint32_t m[8], sg[8], lo, hi;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       m[i] = raw[i] & 0x7FFFFFFFu;
       sg[i] = raw[i] >> 31;
     }
-    encode_wide_group<false, BITS, FMT == MXP_FMT_MXFP6P || FMT == MXP_FMT_MXFP8P>(raw, m, sg, part, lo, hi, sb, idx);
-    if (BITS == 8) {
+    if constexpr (FMT <= MXP_FMT_MXFP6P) {
+      encode_fp6_group<false, PLUS>(raw, m, part, lo, hi, sb, idx);
+      if (part < 3u) *reinterpret_cast<u32x2*>(a.elems + blk * 24 + part * 8) = u32x2{lo, hi};
+    } else {
+      encode_wide_group<false, 8, PLUS>(raw, m, sg, part, lo, hi, sb, idx);
       *reinterpret_cast<u32x2*>(a.elems + blk * 32 + part * 8) = u32x2{lo, hi};
-    } else {                                                         // 48 bits a lane: lane 0 -> d0; 1 -> d1, d2; 2 -> d3; 3 -> d4, d5
-      const uint32_t left_hi = dpp_mov<kQuadFromEven>(hi);
-      uint32_t* out = reinterpret_cast<uint32_t*>(a.elems + blk * 24) + (part >> 1) * 3u;
-      if (part & 1u) {
-        out[1] = (left_hi & 0xFFFFu) | (lo << 16);
-        out[2] = (lo >> 16) | (hi << 16);
-      } else {
-        out[0] = lo;
-      }
     }
   }
   if (part == 0u) {

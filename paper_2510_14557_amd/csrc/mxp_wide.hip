@@ -124,13 +124,11 @@ typedef float v16f __attribute__((ext_vector_type(16)));
 typedef uint32_t v6u __attribute__((ext_vector_type(6)));
 typedef float v2f __attribute__((ext_vector_type(2)));
 typedef float v32f __attribute__((ext_vector_type(32)));
-constexpr int kQuadLane0 = 0x00, kQuadLane1 = 0x55, kQuadLane2 = 0xAA, kQuadLane3 = 0xFF;   // quad_perm broadcasts
 
 template <bool BF16, bool PLUS, bool DENSE>
 __global__ void __launch_bounds__(256) quantize_fp6_kernel(const void* __restrict__ src, int64_t nbk, int64_t ld, int64_t nq,
                                                            uint8_t* __restrict__ elems, uint8_t* __restrict__ scales,
                                                            uint8_t* __restrict__ bm_idx) {
-  using F = Elem<6>;
   constexpr int NW = BF16 ? 4 : 8;                  // dwords a lane loads
   const uint32_t part = threadIdx.x & 3u;
   const int64_t stride = (int64_t)gridDim.x * 256;
@@ -160,67 +158,8 @@ __global__ void __launch_bounds__(256) quantize_fp6_kernel(const void* __restric
         a[i] = t[i] & 0x7FFFFFFFu;
       }
     }
-    uint32_t mx = a[0];
-#pragma unroll
-    for (int i = 1; i < 8; ++i) mx = umax(mx, a[i]);
-    mx = umax(mx, dpp_mov<kQuadSwap1>(mx));
-    mx = umax(mx, dpp_mov<kQuadSwap2>(mx));
-    uint32_t pos = 32u;                             // lowest position holding the maximum
-#pragma unroll
-    for (int i = 7; i >= 0; --i) pos = a[i] == mx ? part * 8u + (uint32_t)i : pos;
-    pos = umin(pos, dpp_mov<kQuadSwap1>(pos));
-    pos = umin(pos, dpp_mov<kQuadSwap2>(pos));
-    const uint32_t E = mx >> 23;
-    const bool flush = E <= (uint32_t)F::EMAX, nonfinite = E == 255u;
-    const int sbyte = (int)E - F::EMAX;
-    const float X = __uint_as_float((uint32_t)(sbyte > 0 ? sbyte : 1) << 23);
-    // the whole block in every lane of the quad
-    uint32_t all[4 * NW];
-#pragma unroll
-    for (int j = 0; j < NW; ++j) {
-      all[0 * NW + j] = dpp_mov<kQuadLane0>(w[j]);
-      all[1 * NW + j] = dpp_mov<kQuadLane1>(w[j]);
-      all[2 * NW + j] = dpp_mov<kQuadLane2>(w[j]);
-      all[3 * NW + j] = dpp_mov<kQuadLane3>(w[j]);
-    }
-    v6u r;
-    if (BF16) {
-      union { uint32_t u[16]; v32bf v; } c;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) c.u[i] = all[i];
-      r = __builtin_amdgcn_cvt_scalef32_pk32_fp6_bf16(c.v, X);
-    } else {
-      v16f lo16, hi16;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {                   // the two sources are interleaved: code 2i from the first, 2i + 1 from the second
-        lo16[i] = __uint_as_float(all[2 * i]);
-        hi16[i] = __uint_as_float(all[2 * i + 1]);
-      }
-      r = __builtin_amdgcn_cvt_scalef32_2xpk16_fp6_f32(lo16, hi16, X);
-    }
-    // this lane's share: dwords 2 part, 2 part + 1 (lane 3 stores nothing)
-    uint32_t s0 = part == 0u ? r[0] : (part == 1u ? r[2] : r[4]);
-    uint32_t s1 = part == 0u ? r[1] : (part == 1u ? r[3] : r[5]);
-    if (PLUS) {
-      // the BM's magnitude mmmmm at bit 6 pos of the block's string = bit rel of this share (may hang over either edge); its
-      // sign is there already: a BM is at least 4 X, and the conversion keeps the sign
-      const uint32_t code = bm_code<6>(mx);
-      const int rel = (int)(6u * pos) - 64 * (int)part;
-      uint64_t share = ((uint64_t)s1 << 32) | s0;
-      if (rel > -6 && rel < 64) {
-        const uint64_t m = rel >= 0 ? ((uint64_t)0x1Fu << rel) : ((uint64_t)0x1Fu >> (-rel));
-        const uint64_t c = rel >= 0 ? ((uint64_t)code << rel) : ((uint64_t)code >> (-rel));
-        share = (share & ~m) | c;
-      }
-      s0 = (uint32_t)share;
-      s1 = (uint32_t)(share >> 32);
-    }
-    uint32_t sb = (uint32_t)sbyte, idx = pos;
-    if (flush || nonfinite) {
-      s0 = s1 = 0;
-      idx = 0;
-      sb = nonfinite ? 255u : 0u;
-    }
+    uint32_t s0, s1, sb, idx;
+    encode_fp6_group<BF16, PLUS>(w, a, part, s0, s1, sb, idx);
     if (q < nq && part < 3u) *reinterpret_cast<u32x2*>(elems + g * 24 + part * 8) = u32x2{s0, s1};
     if (part == 0u && q < nq) {
       scales[g] = (uint8_t)sb;
