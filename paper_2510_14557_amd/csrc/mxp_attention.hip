@@ -56,6 +56,9 @@ struct AttnArgs {
 
 constexpr int kWaves = 4;                                     // of a workgroup
 constexpr float kInf = __builtin_inff();
+// The reference of a row's weights follows its running maximum only where that is more than 2^kGrowth ahead: a weight is then at
+// most 2^kGrowth instead of 1, with the same relative error in bf16 and in the fp32 sums, and most tiles of tokens need no rescaling.
+constexpr float kGrowth = 8.0f;
 __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ float zero_if_none(float m) { return m == -kInf ? 0.0f : m; }   // 2^(x - m) where nothing was seen yet
 
@@ -258,10 +261,10 @@ __device__ __forceinline__ void finish_row(const AttnArgs& a, int64_t part_row, 
 
 // ---- dealing out the work --------------------------------------------------------------------------------------------
 // How a call's work is dealt to workgroups where it is split: in units of tokens, counted over sequences, their key-value heads and
-// their tiles of rows.  Workgroup g of n takes units [g total / n, (g + 1) total / n), whatever
-// the lengths are: a run of rows' tokens that begins or ends inside one (seq, head, tile).  Those two leave parts in the workspace, at
-// 2 g (begun by another workgroup) and 2 g + 1 (begun here); what lies between them is finished here.  The workgroup that begins
-// rows that others go on with records so, and attn_join_kernel adds the parts of its workgroup and of those behind it.
+// their tiles of rows.  A workgroup's share, g of n, is units [g total / n, (g + 1) total / n), whatever the lengths are: it may begin
+// and end inside a tile of rows.  Those two leave parts in the workspace, at 2 g (begun by another share) and 2 g + 1 (begun in this
+// one); what lies between them is finished here.  The share that begins rows that others go on with records so, and
+// attn_join_kernel adds its part and those of the shares behind it.
 struct Load {
   int first, end, units, tiles;                              // tokens that any row sees, in units; tiles of rows
   int64_t total;                                             // units x tiles x key-value heads
@@ -278,10 +281,10 @@ struct Load {
 };
 struct Share {
   int64_t begin, end, total;                                 // this workgroup's units; all
-  int seq, item, off, n;                                     // where `begin` is: sequence, item in it, unit of the item; workgroups that have any
+  int seq, item, off, n, me;                                 // where `begin` is: sequence, item in it, unit of the item; shares; the number of this one
   __device__ __forceinline__ int workgroup_of(int64_t unit) const { return (int)(((unit + 1) * n - 1) / total); }
 };
-__device__ __forceinline__ void find_share(const AttnArgs& a, int rows, int unit, int least, Share& share, int64_t (&wave_sum)[kWaves]) {
+__device__ __forceinline__ void find_share(const AttnArgs& a, int rows, int unit, int least, bool near, Share& share, int64_t (&wave_sum)[kWaves]) {
   const int each = (a.n_seq + 64 * kWaves - 1) / (64 * kWaves), lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int s0 = (int)threadIdx.x * each, s1 = s0 + each < a.n_seq ? s0 + each : a.n_seq;
   int64_t mine = 0;
@@ -306,8 +309,12 @@ __device__ __forceinline__ void find_share(const AttnArgs& a, int rows, int unit
   }
   const int64_t most = (total + least - 1) / least;
   const int64_t n = most < (int64_t)gridDim.x ? most : (int64_t)gridDim.x;
-  if ((int64_t)blockIdx.x < n) {
-    const int64_t begin = blockIdx.x * total / n, end = (blockIdx.x + 1) * total / n;
+  // near: neighbouring shares, which then often read the same tokens, on one XCD (workgroups go to the eight of them in turn).  Chunks
+  // behind long contexts 187 -> 184 us; few rows, whose tokens nobody else reads, lose 3 % by it.
+  const int64_t eights = near ? n >> 3 : 0, id = blockIdx.x, g = id < 8 * eights ? (id & 7) * eights + (id >> 3) : id;
+  if (threadIdx.x == 0) share.me = (int)g;
+  if (g < n) {
+    const int64_t begin = g * total / n, end = (g + 1) * total / n;
     int64_t before = upto - mine;
     if (begin >= before && begin < upto)                     // one lane: the sequence is one of its own
       for (int s = s0; s < s1; ++s) {
@@ -330,10 +337,10 @@ __device__ __forceinline__ void find_share(const AttnArgs& a, int rows, int unit
 
 // The rows and tokens that a workgroup goes over, one run after another: its share, or (a.direct) whole tiles of rows.
 struct Walk {
-  int seq, kv_head = 0, tile = 0, item = 0, off = 0;
+  int seq, kv_head = 0, tile = 0, item = 0, off = 0, me = 0;
   int64_t left = 0, end = 0;
   int part = -1;                                             // where a run's result goes: out, or among the parts
-  __device__ __forceinline__ Walk(const AttnArgs& a, int rows, int unit, int least, Share& share, int64_t (&wave_sum)[kWaves]) {
+  __device__ __forceinline__ Walk(const AttnArgs& a, int rows, int unit, int least, bool near, Share& share, int64_t (&wave_sum)[kWaves]) {
     if (a.direct) {
       // key-value head fastest (consecutive workgroups go to different XCDs: with 8 heads an XCD's cache has one to hold), then tile
       // of rows, the longest first, then sequence
@@ -343,8 +350,9 @@ struct Walk {
       tile = (int)(id % (uint32_t)a.row_tiles);
       seq = (int)(id / (uint32_t)a.row_tiles);
     } else {
-      find_share(a, rows, unit, least, share, wave_sum);
-      if (threadIdx.x == 0) a.joins[4 * blockIdx.x] = -1;
+      find_share(a, rows, unit, least, near, share, wave_sum);
+      me = uniform(share.me);
+      if (threadIdx.x == 0) a.joins[4 * me] = -1;
       end = uniform(share.end);
       left = end - uniform(share.begin);
       seq = uniform(share.seq);
@@ -377,9 +385,9 @@ struct Walk {
       if (till < load.units) to = load.first + till * unit;
       part = -1;
       if (off > 0 || till < load.units) {
-        part = 2 * (int)blockIdx.x + (off == 0 ? 1 : 0);
+        part = 2 * me + (off == 0 ? 1 : 0);
         if (off == 0 && threadIdx.x == 0) {                  // the first part of these rows: the join goes on to the last one's workgroup
-          int32_t* const j = a.joins + 4 * blockIdx.x;
+          int32_t* const j = a.joins + 4 * me;
           j[1] = kv_head;
           j[2] = r0;
           j[3] = share.workgroup_of(end - left + load.units - 1);
@@ -528,7 +536,7 @@ __global__ void __launch_bounds__(64 * WAVES, few_waves_per_simd(D, NT)) attn_fe
   constexpr int ROWS = 16 * NT;
   __shared__ Share share;
   __shared__ int64_t wave_sum[kWaves];
-  for (Walk walk(a, ROWS, kFewUnit, kFewLeast, share, wave_sum);;) {
+  for (Walk walk(a, ROWS, kFewUnit, kFewLeast, false, share, wave_sum);;) {
     if (!walk.more(a)) break;
     const Sequence s(a, walk.seq);
     if (!walk.more(a, s, ROWS)) break;
@@ -642,14 +650,14 @@ __global__ void __launch_bounds__(64 * WAVES, few_waves_per_simd(D, NT)) attn_fe
       for (int t = 0; t < NT; ++t) {
         float mx = fmaxf(fmaxf(fmaxf(sc[t][0][0], sc[t][0][1]), fmaxf(sc[t][0][2], sc[t][0][3])), fmaxf(fmaxf(sc[t][1][0], sc[t][1][1]), fmaxf(sc[t][1][2], sc[t][1][3])));
         mx = fmaxf(m[t], max_across_32(max_across_16(mx)));
-        const float base = zero_if_none(mx) * a.scale;
-        if (__any(mx != m[t])) {
-          const float fade = exp2_of(m[t] * a.scale - base);
+        if (__any((mx - m[t]) * a.scale > kGrowth)) {
+          const float fade = exp2_of((m[t] - zero_if_none(mx)) * a.scale);
           l[t] *= fade;
 #pragma unroll
           for (int d = 0; d < D / 16; ++d) o[t][d] *= fade;
           m[t] = mx;
         }
+        const float base = zero_if_none(m[t]) * a.scale;
         l[t] += weights<TERMS>(sc[t][0], sc[t][1], a.scale, base, p[t]);
       }
       const uint32_t v_at = formed_at_use(token_at<D>(4 * quarter + (col >> 2)) ^ (8u * (col & 3)));
@@ -726,8 +734,33 @@ __global__ void __launch_bounds__(64 * WAVES, few_waves_per_simd(D, NT)) attn_fe
   }
 }
 
-// The joins that Share records, `each` workgroups' records per workgroup here: a row at a time by a wavefront, or by the workgroup
-// where the parts are many.
+// Four values of a row per lane, for at most kFewParts parts: every lane forms the weights by itself.
+constexpr int kFewParts = 4;
+template <class PartAt>
+__device__ __forceinline__ void join_values(const AttnArgs& a, int parts, PartAt part_at, int64_t row, int head, int d) {
+  float m[kFewParts], l[kFewParts], top = -kInf, sum = 0.0f;
+  f32x4 x[kFewParts], out = {0, 0, 0, 0};
+#pragma unroll
+  for (int p = 0; p < kFewParts; ++p) {
+    const int64_t at = part_at(p < parts ? p : 0);
+    m[p] = p < parts ? a.part_ml[2 * at] : -kInf;
+    l[p] = p < parts ? a.part_ml[2 * at + 1] : 0.0f;
+    x[p] = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(a.part_o + at * a.g.D + d));
+  }
+#pragma unroll
+  for (int p = 0; p < kFewParts; ++p) top = fmaxf(top, m[p]);
+#pragma unroll
+  for (int p = 0; p < kFewParts; ++p) {
+    if (l[p] == 0.0f) continue;
+    const float f = exp2_of(m[p] - zero_if_none(top));
+    sum += l[p] * f;
+    out += x[p] * f;
+  }
+  store_out(a, row, head, d, sum == 0.0f ? f32x4{0, 0, 0, 0} : out / sum);
+  if (d == 0 && a.lse) a.lse[row * a.heads + head] = lse_of(top, sum);
+}
+
+// The joins that Share records, `each` workgroups' records per workgroup here, in the one of three ways that fits the parts.
 __global__ void __launch_bounds__(256) attn_join_kernel(const AttnArgs a, int rows_per_tile, int n_records, int each) {
   __shared__ JoinRoom room;
   const int lane = threadIdx.x & 63, first = (int)blockIdx.x * each;
@@ -737,6 +770,16 @@ __global__ void __launch_bounds__(256) attn_join_kernel(const AttnArgs a, int ro
     const int32_t* const j = a.joins + 4 * g;
     const Sequence s(a, j[0]);
     const int kv_head = j[1], r0 = j[2], parts = j[3] - g + 1, R = s.n * a.group;
+    if (parts <= kFewParts) {
+      const int across = a.g.D >> 2;
+      for (int i = (int)blockIdx.y * 256 + (int)threadIdx.x; i < rows_per_tile * across; i += 256 * (int)gridDim.y) {
+        const int row = i / across, r = r0 + row, query = r / a.group;
+        if (r >= R) break;
+        join_values(a, parts, [&](int p) { return ((int64_t)2 * (g + p) + (p == 0 ? 1 : 0)) * rows_per_tile + row; }, s.q0 + query,
+                    kv_head * a.group + r - query * a.group, 4 * (i - row * across));
+      }
+      continue;
+    }
     const bool by_wave = parts <= 64;
     const int step = (by_wave ? 4 : 1) * (int)gridDim.y;
     for (int row = by_wave ? (int)blockIdx.y * 4 + (int)(threadIdx.x >> 6) : (int)blockIdx.y; row < rows_per_tile && r0 + row < R; row += step) {
@@ -769,7 +812,7 @@ __global__ void __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) attn_many_kerne
   const auto job_block = [&](int k, int who) { return D == 64 ? who >> 5 : 4 * (k >> 1) + (who >> 4); };
   __shared__ Share share;
   __shared__ int64_t wave_sum[kWaves];
-  for (Walk walk(a, kManyRows, kManyTokens, kManyLeast, share, wave_sum);;) {
+  for (Walk walk(a, kManyRows, kManyTokens, kManyLeast, true, share, wave_sum);;) {
     if (!walk.more(a)) break;
     const Sequence s(a, walk.seq);
     if (!walk.more(a, s, kManyRows)) break;
@@ -880,14 +923,14 @@ __global__ void __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) attn_many_kerne
 #pragma unroll
           for (int j = 0; j < 16; ++j) mx = fmaxf(mx, sc[h][j]);
         mx = fmaxf(m, max_across_32(mx));
-        const float base = zero_if_none(mx) * a.scale;
-        if (__any(mx != m)) {
-          const float f = exp2_of(m * a.scale - base);
-          l *= f;
+        if (__any((mx - m) * a.scale > kGrowth)) {
+          const float fade = exp2_of((m - zero_if_none(mx)) * a.scale);
+          l *= fade;
 #pragma unroll
-          for (int d = 0; d < DB; ++d) o[d] *= f;
+          for (int d = 0; d < DB; ++d) o[d] *= fade;
           m = mx;
         }
+        const float base = zero_if_none(m) * a.scale;
 #pragma unroll
         for (int b = 0; b < 4; ++b) {                        // 16 tokens: registers 8 (b % 2) ... + 7 of half b / 2
           Operand p[TERMS];
@@ -1075,12 +1118,13 @@ extern "C" int mxp_attention(const void* Q, int q_dtype, int64_t ld_q, int64_t r
 #undef MXP_ATTN_T
   if (!p.direct) {
     // Where many parts are to be joined there are few records: 16 of them and one row per workgroup (one sequence of 131000 tokens,
-    // 8 joins of 128 parts: 14.6 -> 7.8 us against a record each); else a record per workgroup and a row per wavefront.
+    // 8 joins of 128 parts: 14.6 -> 7.8 us against a record each); else a record per workgroup, of 16 rows, as few parts take them.
     int64_t most = (max_q < rows ? max_q : rows) * a.group;
     most = most < 1 ? 1 : most < p.rows ? most : p.rows;
     const bool many_parts = p.wgs > 32 * n_seq * kv_heads * p.row_tiles;
     const int each = many_parts ? 16 : 1;
-    hipLaunchKernelGGL(attn_join_kernel, dim3((unsigned)((p.wgs + each - 1) / each), (unsigned)(many_parts ? most : (most + 3) / 4)), dim3(256), 0, s, a, p.rows,
+    const int64_t y = many_parts ? most : (most + 15) / 16;
+    hipLaunchKernelGGL(attn_join_kernel, dim3((unsigned)((p.wgs + each - 1) / each), (unsigned)y), dim3(256), 0, s, a, p.rows,
                        (int)p.wgs, each);
   }
   return launch_status();
