@@ -152,6 +152,12 @@ struct Span {
   }
 };
 
+// how many tokens there are from `first` to `last`, before `end`
+__device__ __forceinline__ uint32_t tokens_from_to(int first, int last, int end) {
+  const int n = (last < end ? last + 1 : end) - first;
+  return n > 0 ? (uint32_t)n : 0u;
+}
+
 // The page of a token: its number, or -1 where it has none
 __device__ __forceinline__ int32_t page_of(const AttnArgs& a, const Sequence& s, int64_t t) {
   const int64_t j = t >> a.g.page_shift;
@@ -279,6 +285,12 @@ struct Load {
     total = (int64_t)units * tiles * a.g.kv_heads;
   }
 };
+// Shares of so many units, each at least `least`, or half of that while they are fewer than the compute units (one sequence of 2048
+// tokens, 8 heads: 19.0 us with four, 15.8 with two; 16 such sequences 24 with four, 29 with two).
+__host__ __device__ inline int64_t shares_of(int64_t units, int64_t least) {
+  const int64_t n = (units + least - 1) / least, twice = (units + least / 2 - 1) / (least / 2);
+  return n >= kNumCU ? n : twice < kNumCU ? twice : kNumCU;
+}
 struct Share {
   int64_t begin, end, total;                                 // this workgroup's units; all
   int seq, item, off, n, me;                                 // where `begin` is: sequence, item in it, unit of the item; shares; the number of this one
@@ -307,8 +319,7 @@ __device__ __forceinline__ void find_share(const AttnArgs& a, int rows, int unit
     if (w < wave) upto += wave_sum[w];
     total += wave_sum[w];
   }
-  const int64_t most = (total + least - 1) / least;
-  const int64_t n = most < (int64_t)gridDim.x ? most : (int64_t)gridDim.x;
+  const int64_t most = shares_of(total, least), n = most < (int64_t)gridDim.x ? most : (int64_t)gridDim.x;
   // near: neighbouring shares, which then often read the same tokens, on one XCD (workgroups go to the eight of them in turn).  Chunks
   // behind long contexts 187 -> 184 us; few rows, whose tokens nobody else reads, lose 3 % by it.
   const int64_t eights = near ? n >> 3 : 0, id = blockIdx.x, g = id < 8 * eights ? (id & 7) * eights + (id >> 3) : id;
@@ -530,9 +541,11 @@ __global__ void __launch_bounds__(64 * WAVES, few_waves_per_simd(D, NT)) attn_fe
   const int col = lane & 15, quarter = lane >> 4;
   uint8_t* const patch = lds + wave * PATCH;                 // a tile's keys, then its values
   float* const ml = reinterpret_cast<float*>(lds + WAVES * PATCH);   // [wave][row][2]
-  // this lane's blocks of a tile: its token (16 lanes in a row have 16 tokens: their stores fall on all banks), its block of the token
-  const auto token_of = [&](int i) { return D == 256 ? 16 * (i >> 1) + (lane & 15) : LANE_TOKENS * i + (lane & (LANE_TOKENS - 1)); };
-  const auto block_of = [&](int i) { return D == 256 ? 4 * (i & 1) + (lane >> 4) : lane / LANE_TOKENS; };
+  // This lane's blocks of a tile: the first one's token (16 lanes in a row have 16 tokens: their stores fall on all banks) and its block
+  // of the token; how far on the i-th is
+  const int lane_token = lane & (LANE_TOKENS - 1), lane_block = lane / LANE_TOKENS;
+  const auto tokens_on = [](int i) { return D == 256 ? 16 * (i >> 1) : LANE_TOKENS * i; };
+  const auto blocks_on = [](int i) { return D == 256 ? 4 * (i & 1) : 0; };
   constexpr int ROWS = 16 * NT;
   __shared__ Share share;
   __shared__ int64_t wave_sum[kWaves];
@@ -546,13 +559,14 @@ __global__ void __launch_bounds__(64 * WAVES, few_waves_per_simd(D, NT)) attn_fe
     const int R = s.n * a.group, kv_head = walk.kv_head, part = walk.part;
     // this lane's rows, as operands of the first product: channels 32 st + 8 quarter ... + 7
     Operand q[NT][DB];
-    int first[NT], last[NT];
+    int first[NT];                                           // what a row sees of the span: from here,
+    uint32_t seen[NT];                                       // so many tokens
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
       const int r = r0 + 16 * t + col, i = r / a.group;
       const bool there = r < R;
-      first[t] = there ? s.first(a, i) : 1;
-      last[t] = there ? s.last(a, i) : 0;
+      first[t] = s.first(a, i);
+      seen[t] = there ? tokens_from_to(first[t], s.last(a, i), span.end) : 0u;
       const uint16_t* p = a.q + (s.q0 + (there ? i : 0)) * a.ld_q + (int64_t)(kv_head * a.group + (there ? r - i * a.group : 0)) * D + 8 * quarter;
 #pragma unroll
       for (int st = 0; st < DB; ++st) {
@@ -590,21 +604,21 @@ __global__ void __launch_bounds__(64 * WAVES, few_waves_per_simd(D, NT)) attn_fe
       ++fetched;
 #pragma unroll
       for (int i = 0; i < NB; ++i) {
-        const int token = token_of(i);
-        const bool second = D == 64 ? token >= 16 : i >= NB / 2;
+        const bool second = D == 64 ? lane_token >= 16 : tokens_on(i) >= 16;
         const uint8_t* rec = second ? p1.rec : p0.rec;
-        const int row = second ? p1.at + (token & 15) : p0.at + token;
-        f.k[i] = load_block<D, MODE, true>(rec, a.g, row, block_of(i));
-        f.v[i] = load_block<D, MODE, true>(rec + a.g.part_bytes, a.g, row, block_of(i));
+        const int row = (second ? p1.at : p0.at) + (lane_token & 15);
+        f.k[i] = load_block<D, MODE, true>(rec, a.g, row, lane_block + blocks_on(i));
+        f.v[i] = load_block<D, MODE, true>(rec + a.g.part_bytes, a.g, row, lane_block + blocks_on(i));
       }
     };
+    const uint32_t lane_at = token_at<D>(lane_token) ^ (64u * lane_block);
     const auto take = [&](Fetched& f, int t0) {
       if (t0 >= span.end) return;
       const bool h0 = f.held0, h1 = f.held1;
       uint64_t nan[NB];                                      // lanes whose block of V is NaN: zeros here, put in behind the product
       uint64_t any = 0;
 #pragma unroll
-      for (int i = 0; i < NB; ++i) expand<MODE>(f.k[i], false, patch, formed_at_use(token_at<D>(token_of(i)) ^ (64u * block_of(i))));
+      for (int i = 0; i < NB; ++i) expand<MODE>(f.k[i], false, patch + 2 * D * tokens_on(i), formed_at_use(lane_at) ^ (64u * blocks_on(i)));
       __builtin_amdgcn_wave_barrier();
       f32x4 sc[NT][2];
       const uint32_t k_at = formed_at_use(token_at<D>(col) ^ (16u * quarter));
@@ -625,25 +639,24 @@ __global__ void __launch_bounds__(64 * WAVES, few_waves_per_simd(D, NT)) attn_fe
       __builtin_amdgcn_wave_barrier();                       // (the reads above come first: LDS serves a wavefront in order)
 #pragma unroll
       for (int i = 0; i < NB; ++i) {
-        const int token = token_of(i);
+        const int token = lane_token + tokens_on(i);
         const bool dead = t0 + token >= span.end || !(token >= 16 ? h1 : h0);
         nan[i] = __ballot(f.v[i].scale == 255u && !dead);
         any |= nan[i];
-        expand<MODE>(f.v[i], dead || f.v[i].scale == 255u, patch, formed_at_use(token_at<D>(token) ^ (64u * block_of(i))));
+        expand<MODE>(f.v[i], dead || f.v[i].scale == 255u, patch + 2 * D * tokens_on(i), formed_at_use(lane_at) ^ (64u * blocks_on(i)));
       }
       __builtin_amdgcn_wave_barrier();
       fetch(f, t0 + kFewAhead * 32 * WAVES);
       const bool whole = h0 && h1 && t0 >= all_from && t0 + 31 <= all_to && t0 + 32 <= span.end;   // (uniform)
       if (!whole) {
 #pragma unroll
-        for (int t = 0; t < NT; ++t)
+        for (int t = 0; t < NT; ++t) {
+          const uint32_t from_first = (uint32_t)(t0 + 4 * quarter - first[t]);
 #pragma unroll
           for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const int tok = t0 + 16 * h + 4 * quarter + i;
-              sc[t][h][i] = tok >= first[t] && tok <= last[t] && tok < span.end && (h ? h1 : h0) ? sc[t][h][i] : -kInf;
-            }
+            for (int i = 0; i < 4; ++i) sc[t][h][i] = from_first + 16u * h + i < seen[t] && (h ? h1 : h0) ? sc[t][h][i] : -kInf;
+        }
       }
       Operand p[NT][TERMS];
 #pragma unroll
@@ -679,14 +692,14 @@ __global__ void __launch_bounds__(64 * WAVES, few_waves_per_simd(D, NT)) attn_fe
 #pragma unroll
           for (int k = 1; k < NB; ++k) left = i == k ? nan[k] : left;
           for (; left; left &= left - 1) {
-            const int who = __builtin_ctzll(left), tok = t0 + __builtin_amdgcn_readlane(token_of(i), who), blk = __builtin_amdgcn_readlane(block_of(i), who);
+            const int who = __builtin_ctzll(left), tok = t0 + (who & (LANE_TOKENS - 1)) + tokens_on(i), blk = who / LANE_TOKENS + blocks_on(i);
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
-              const bool seen = tok >= first[t] && tok <= last[t];
+              const bool sees = (uint32_t)(tok - first[t]) < seen[t];
 #pragma unroll
               for (int d = 0; d < D / 16; ++d)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) o[t][d][j] = seen && d / 2 == blk ? __uint_as_float(0x7FC00000u) : o[t][d][j];
+                for (int j = 0; j < 4; ++j) o[t][d][j] = sees && d / 2 == blk ? __uint_as_float(0x7FC00000u) : o[t][d][j];
             }
           }
         }
@@ -822,7 +835,8 @@ __global__ void __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) attn_many_kerne
     const int R = s.n * a.group, kv_head = walk.kv_head, part = walk.part;
     const int r = r0 + 32 * wave + col, i = r / a.group;
     const bool there = r < R;
-    const int first = there ? s.first(a, i) : 1, last = there ? s.last(a, i) : 0;
+    const int first = s.first(a, i);                         // what the row sees of the span: from here,
+    const uint32_t seen = there ? tokens_from_to(first, s.last(a, i), span.end) : 0u;   // so many tokens
     const int head = kv_head * a.group + (there ? r - i * a.group : 0);
     Operand q[D / 16];
     {
@@ -909,13 +923,17 @@ __global__ void __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) attn_many_kerne
         }
         const bool whole = held == 15u && t0 >= all_from && t0 + kManyTokens - 1 <= all_to && t0 + kManyTokens <= span.end;
         if (!whole) {
+          const uint32_t from_first = (uint32_t)(t0 + 4 * half - first);
 #pragma unroll
           for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int j = 0; j < 16; ++j) {
-              const int tok = t0 + 32 * h + 8 * (j >> 2) + 4 * half + (j & 3);
-              sc[h][j] = tok >= first && tok <= last && tok < span.end && ((held >> (2 * h + (j >> 3))) & 1u) ? sc[h][j] : -kInf;
-            }
+            for (int j = 0; j < 16; ++j) sc[h][j] = from_first + (32u * h + 8 * (j >> 2) + (j & 3)) < seen ? sc[h][j] : -kInf;
+          if (held != 15u) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+              for (int j = 0; j < 16; ++j) sc[h][j] = (held >> (2 * h + (j >> 3))) & 1u ? sc[h][j] : -kInf;
+          }
         }
         float mx = -kInf;
 #pragma unroll
@@ -955,11 +973,11 @@ __global__ void __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) attn_many_kerne
           for (int k = 0; k < kWaves * JOBS; ++k)
             for (uint64_t left = nans[buf * kWaves * JOBS + k]; left; left &= left - 1) {
               const int who = __builtin_ctzll(left), tok = t0 + job_token(k / JOBS, who), blk = job_block(k % JOBS, who);
-              const bool seen = tok >= first && tok <= last;
+              const bool sees = (uint32_t)(tok - first) < seen;
 #pragma unroll
               for (int d = 0; d < DB; ++d)
 #pragma unroll
-                for (int j = 0; j < 16; ++j) o[d][j] = seen && d == blk ? __uint_as_float(0x7FC00000u) : o[d][j];
+                for (int j = 0; j < 16; ++j) o[d][j] = sees && d == blk ? __uint_as_float(0x7FC00000u) : o[d][j];
             }
         }
       }
@@ -990,7 +1008,9 @@ struct Plan {
 };
 
 // Sequences of at most so many tokens are not dealt out in parts: a workgroup goes over them in less than the parts' join takes.
-constexpr int64_t kFewDirect = 2048, kManyDirect = 1024;
+// (Few rows, us whole | dealt out: 8 tiles of rows of 1024 tokens 17.1 | 15.9, of 2048 22.7 | 15.8; 128 of 1024 17.5 | 19.4, of 2048
+// 23.8 | 29; 320 of 2048 40 | 44.)
+constexpr int64_t kFewDirect = 2048, kFewestDirect = 512, kManyDirect = 1024;
 
 // Which kernel (up to 32 rows of a key-value head: attn_few_kernel), and whether a workgroup takes whole tiles of rows or a share of
 // all tokens.  Whole tiles where sequences are short, where workgroups come in several rounds anyhow (they then even out among
@@ -1008,9 +1028,9 @@ Plan plan_for(int64_t n_seq, int64_t max_q, int64_t max_kv, int64_t heads, int64
   const int64_t room = (int64_t)kNumCU * (p.many ? (D == 256 ? 1 : 2) : few_waves_per_simd((int)D, p.rows / 16));   // workgroups that run at once
   const int64_t unit = p.many ? kManyTokens : kFewUnit, least = p.many ? kManyLeast : kFewLeast, units = items * ((len + unit - 1) / unit);
   const bool prompt = p.many && causal && 2 * max_q > len && 2 * items > room;
-  p.direct = len <= (p.many ? kManyDirect : kFewDirect) || items >= 4 * room || prompt;
+  p.direct = len <= (p.many ? kManyDirect : items > 64 ? kFewDirect : kFewestDirect) || items >= 4 * room || prompt;
   p.alone = !p.many && p.direct && items <= kNumCU;
-  p.wgs = p.direct ? items : units < least * room ? (units + least - 1) / least : room;
+  p.wgs = p.direct ? items : shares_of(units, least) < room ? shares_of(units, least) : room;
   return p;
 }
 
@@ -1117,13 +1137,14 @@ extern "C" int mxp_attention(const void* Q, int q_dtype, int64_t ld_q, int64_t r
 #undef MXP_ATTN_M
 #undef MXP_ATTN_T
   if (!p.direct) {
-    // Where many parts are to be joined there are few records: 16 of them and one row per workgroup (one sequence of 131000 tokens,
-    // 8 joins of 128 parts: 14.6 -> 7.8 us against a record each); else a record per workgroup, of 16 rows, as few parts take them.
+    // About so many parts a join: above 32 there are few records, 16 of them and one row per workgroup (one sequence of 131000 tokens,
+    // 8 joins of 128 parts: 14.6 -> 7.8 us against a record each); else a record per workgroup, one row per wavefront or, as a few
+    // parts take them, 16 rows.
+    const int64_t parts_each = p.wgs / (n_seq * kv_heads * p.row_tiles);
     int64_t most = (max_q < rows ? max_q : rows) * a.group;
     most = most < 1 ? 1 : most < p.rows ? most : p.rows;
-    const bool many_parts = p.wgs > 32 * n_seq * kv_heads * p.row_tiles;
-    const int each = many_parts ? 16 : 1;
-    const int64_t y = many_parts ? most : (most + 15) / 16;
+    const int each = parts_each >= 32 ? 16 : 1;
+    const int64_t y = parts_each >= 32 ? most : parts_each >= kFewParts ? (most + 3) / 4 : (most + 15) / 16;
     hipLaunchKernelGGL(attn_join_kernel, dim3((unsigned)((p.wgs + each - 1) / each), (unsigned)y), dim3(256), 0, s, a, p.rows,
                        (int)p.wgs, each);
   }
