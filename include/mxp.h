@@ -396,6 +396,7 @@ int mxp_cache_read(const void* cache, int64_t n_pages, int64_t page_tokens, int6
  * kv_len, table and q_start are read on the device only.  max_q and max_kv are the caller's upper bounds on queries and kv_len of a
  * sequence: they choose launch and splitting, larger sequences are computed all the same, more slowly.
  * rows * heads is at most 2^30 (else MXP_ERR_UNSUPPORTED).
+ * O and lse must not overlap anything that is read.
  * workspace: mxp_attention_workspace_bytes(...) of the same arguments (may be 0), scratch for the parts of split sequences, free
  * again after the call's work on `stream`; a smaller one returns MXP_ERR_WORKSPACE. */
 size_t mxp_attention_workspace_bytes(int64_t n_seq, int64_t rows, int64_t max_q, int64_t max_kv, int64_t heads, int64_t kv_heads,

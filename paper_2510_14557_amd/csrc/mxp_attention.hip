@@ -1015,22 +1015,27 @@ constexpr int64_t kFewDirect = 2048, kFewestDirect = 512, kManyDirect = 1024;
 // Which kernel (up to 32 rows of a key-value head: attn_few_kernel), and whether a workgroup takes whole tiles of rows or a share of
 // all tokens.  Whole tiles where sequences are short, where workgroups come in several rounds anyhow (they then even out among
 // themselves), and for prompts: a tile of theirs sees half the tokens on average, which shares of equal numbers of tokens do not heed.
-Plan plan_for(int64_t n_seq, int64_t max_q, int64_t max_kv, int64_t heads, int64_t kv_heads, int64_t D, int causal, int64_t window) {
+// Shares where the bound on a sequence's queries is far above what most have (a prompt among single queries): whole tiles would
+// be mostly empty workgroups.
+Plan plan_for(int64_t n_seq, int64_t rows, int64_t max_q, int64_t max_kv, int64_t heads, int64_t kv_heads, int64_t D, int causal, int64_t window) {
   Plan p;
-  const int64_t rows = max_q * (heads / kv_heads);           // of one key-value head
-  p.many = rows > 32;
-  p.rows = p.many ? kManyRows : rows > 16 ? 32 : 16;
-  p.row_tiles = (int)((rows + p.rows - 1) / p.rows);
+  max_q = max_q < rows ? max_q : rows;
+  window = window < kMostTokens ? window : kMostTokens;
+  const int64_t group = heads / kv_heads, most = max_q * group;
+  p.many = most > 32;
+  p.rows = p.many ? kManyRows : most > 16 ? 32 : 16;
+  p.row_tiles = (int)((most + p.rows - 1) / p.rows);
   if (p.row_tiles < 1) p.row_tiles = 1;
-  const int64_t items = n_seq * kv_heads * p.row_tiles;
+  const int64_t items = n_seq * kv_heads * p.row_tiles, filled = kv_heads * ((rows * group + p.rows - 1) / p.rows + n_seq), real = items < filled ? items : filled;
   int64_t len = max_kv;                                      // tokens that one tile of rows goes over, at most
   if (window > 0 && window + max_q + 32 < len) len = window + max_q + 32;
   const int64_t room = (int64_t)kNumCU * (p.many ? (D == 256 ? 1 : 2) : few_waves_per_simd((int)D, p.rows / 16));   // workgroups that run at once
-  const int64_t unit = p.many ? kManyTokens : kFewUnit, least = p.many ? kManyLeast : kFewLeast, units = items * ((len + unit - 1) / unit);
+  const int64_t unit = p.many ? kManyTokens : kFewUnit, least = p.many ? kManyLeast : kFewLeast;
+  const int64_t shares = shares_of(real * ((len + unit - 1) / unit), least);
   const bool prompt = p.many && causal && 2 * max_q > len && 2 * items > room;
-  p.direct = len <= (p.many ? kManyDirect : items > 64 ? kFewDirect : kFewestDirect) || items >= 4 * room || prompt;
+  p.direct = items <= 2 * real + room && (len <= (p.many ? kManyDirect : items > 64 ? kFewDirect : kFewestDirect) || items >= 4 * room || prompt);
   p.alone = !p.many && p.direct && items <= kNumCU;
-  p.wgs = p.direct ? items : shares_of(units, least) < room ? shares_of(units, least) : room;
+  p.wgs = p.direct ? items : shares < 1 ? 1 : shares < room ? shares : room;
   return p;
 }
 
@@ -1074,7 +1079,7 @@ bool shapes_fit(int64_t n_seq, int64_t rows, int64_t max_q, int64_t max_kv, int6
 extern "C" size_t mxp_attention_workspace_bytes(int64_t n_seq, int64_t rows, int64_t max_q, int64_t max_kv, int64_t heads, int64_t kv_heads,
                                                 int64_t head_dim, int causal, int64_t window) {
   if (!shapes_fit(n_seq, rows, max_q, max_kv, heads, kv_heads) || n_seq == 0 || rows == 0 || rows * heads > kMostRows || head_dim < 1 || window < 0) return 0;
-  return parts_bytes(plan_for(n_seq, max_q < rows ? max_q : rows, max_kv, heads, kv_heads, head_dim, causal, window), head_dim);
+  return parts_bytes(plan_for(n_seq, rows, max_q, max_kv, heads, kv_heads, head_dim, causal, window), head_dim);
 }
 
 extern "C" int mxp_attention(const void* Q, int q_dtype, int64_t ld_q, int64_t rows, int64_t heads, const int32_t* q_start, const int32_t* kv_len,
@@ -1098,7 +1103,7 @@ extern "C" int mxp_attention(const void* Q, int q_dtype, int64_t ld_q, int64_t r
   if (!aligned16(Q) || !aligned16(O) || !aligned16(cache) || !aligned16(workspace) || ld_q * 2 % 16 != 0 || ld_o * osz % 16 != 0 || off4(q_start) ||
       off4(kv_len) || off4(table) || off4(lse))
     return MXP_ERR_ALIGN;
-  const Plan p = plan_for(n_seq, max_q < rows ? max_q : rows, max_kv, heads, kv_heads, head_dim, causal, window);
+  const Plan p = plan_for(n_seq, rows, max_q, max_kv, heads, kv_heads, head_dim, causal, window);
   if (p.wgs > 2147483647LL) return MXP_ERR_UNSUPPORTED;
   const size_t need = parts_bytes(p, head_dim);
   if (need > 0 && (!workspace || workspace_bytes < need)) return MXP_ERR_WORKSPACE;

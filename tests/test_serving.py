@@ -361,6 +361,30 @@ def test_attention_bounds_are_hints(n):
 
 
 @gpu
+def test_attention_a_prompt_among_single_queries():
+    """One long prompt, many sequences of one query, bounds for the longest, an empty sequence between."""
+    kv, nq = [1500] + [1 + 37 * i for i in range(60)] + [0, 3000], [1500] + [1] * 61 + [5]
+    b = Batch("MXFP4P", 64, 2, 4, 64, kv, nq, seed=21)
+    for out in (torch.bfloat16, torch.float32):
+        b.check(*b.call(out_dtype=out))
+        b.check(*b.call(out_dtype=out, window=100), window=100)
+    b.check(*b.call(causal=False), causal=False)
+
+
+@gpu
+def test_attention_many_sequences():
+    """More sequences than the lanes that add up their lengths, each of its own length, some without queries."""
+    rng = np.random.default_rng(2)
+    kv = [int(x) for x in rng.integers(0, 90, 1500)]
+    kv[700] = 4000
+    b = Batch("MXFP4", 16, 1, 2, 64, kv, [1] * 1500, seed=22)
+    b.check(*b.call())
+    nq = [int(x) for x in rng.integers(0, 3, 1500)]
+    b = Batch("MXFP4", 16, 1, 2, 64, kv, nq, seed=23)
+    b.check(*b.call(max_kv=4000, out_dtype=torch.float32))
+
+
+@gpu
 @pytest.mark.parametrize("n", [1, 3, 70])
 def test_attention_pages_that_are_not_there(n):
     """Entries outside the cache hide their tokens; the last page's tokens behind kv_len hold NaN blocks throughout."""
