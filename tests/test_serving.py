@@ -184,6 +184,36 @@ def test_cache_write_and_read_bit_for_bit(fmt, dt, T, H, D, n):
 
 
 @gpu
+@pytest.mark.parametrize("fmt", FOUR)
+@pytest.mark.parametrize("dt", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("D,H,n", [(64, 7, 20011), (128, 5, 13999), (256, 8, 4099)])
+def test_cache_of_many_rows(fmt, dt, D, H, n):
+    """Enough rows for the launch with several groups per lane: the records are mxp_quantize's bytes, what is read mxp_dequantize's values."""
+    f, T = FMTS[fmt], 64
+    gen = torch.Generator(device="cuda").manual_seed(D)
+    n_pages = n // T + 2
+    slots = torch.randperm(n_pages * T, generator=gen, device="cuda")[:n]
+    k, v = (torch.randn((n, H, D), generator=gen, device="cuda").mul_(torch.exp2(torch.randint(-9, 9, (n, 1, 1), generator=gen, device="cuda").float())).to(dt)
+            for _ in range(2))
+    given = slots.clone()
+    given[::7] = -1
+    cache = mxp.cache_empty(n_pages, T, H, D, f)
+    cache.data.fill_(0xA5)
+    mxp.cache_write(cache, k, v, given)
+    kept = given >= 0
+    for part, x, back in zip((0, 1), (k, v), mxp.cache_read(cache, given, dt)):
+        q = mxp.quantize(x.view(n * H, D), f)
+        at = 0
+        for a, width in zip(q, (D // 2, D // 32, D // 32)[:2 if f == mxp.MXFP4 else 3]):
+            want = torch.full((n_pages * T, H, width), 0xA5, dtype=torch.uint8, device="cuda")
+            want[slots[kept]] = a.view(n, H, width)[kept]
+            got = cache.data[:, :, part, at:at + T * width].reshape(n_pages, H, T, width).transpose(1, 2).reshape(n_pages * T, H, width)
+            assert torch.equal(got, want)
+            at += T * width
+        assert torch.equal(back, torch.where(kept[:, None, None], mxp.dequantize(q, f, dt).view(n, H, D), 0.0))
+
+
+@gpu
 def test_cache_beyond_32_bit_offsets():
     """Pages above 4 GiB: written, read and attended to as the first ones are."""
     T, H, D, f = 256, 8, 128, mxp.MXFP4P
@@ -313,6 +343,18 @@ ODD = [1, 15, 16, 17, 31, 33, 63, 64, 65, 100, 129, 255, 257, 600]
 def test_attention_one_query_each(out, fmt, D, T, H, G):
     b = Batch(fmt, T, H, G, D, ODD, [1] * len(ODD), seed=D + G)
     b.check(*b.call(out_dtype=out))
+
+
+@gpu
+@pytest.mark.parametrize("out", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("fmt", FOUR)
+@pytest.mark.parametrize("G", [3, 20])
+@pytest.mark.parametrize("D", [64, 128, 256])
+def test_attention_every_launch_of_few_rows(out, fmt, G, D):
+    """Up to 16 and up to 32 rows of a head; whole sequences by a workgroup, with a compute unit to itself and not, and shares of them."""
+    for kv in ([100, 300], [2200, 40], [50] * 130):
+        b = Batch(fmt, 32, 2, G, D, kv, [1] * len(kv), seed=G)
+        b.check(*b.call(out_dtype=out))
 
 
 @gpu
