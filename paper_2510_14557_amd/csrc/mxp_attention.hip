@@ -239,6 +239,24 @@ __device__ __forceinline__ void expand(const Block& b, bool drop, uint8_t* tile,
   }
 }
 
+// A block of plain MXFP4 as four operands of eight, in registers.
+__device__ __forceinline__ void expand(const Block& b, Operand (&out)[4]) {
+  const float X = __uint_as_float(b.scale << 23);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const uint32_t c = b.scale == 0u ? 0u : b.code[j];
+    union { bf16x2 v; uint32_t u; } w0, w1, w2, w3;
+    w0.v = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, X, 0);
+    w1.v = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, X, 1);
+    w2.v = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, X, 2);
+    w3.v = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, X, 3);
+    out[j].u[0] = w0.u;
+    out[j].u[1] = w1.u;
+    out[j].u[2] = w2.u;
+    out[j].u[3] = w3.u;
+  }
+}
+
 // four tokens x 16 channels per 16 lanes, transposed: a lane gets four tokens of one channel
 __device__ __forceinline__ s16x4 read_transposed(const uint8_t* p) {
   return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)p);
@@ -526,14 +544,20 @@ template <int D>
 constexpr int few_patch(int nt) { return 64 * D * nt; }      // a tile of 32 tokens (2 D bytes each); 16 nt rows of fp32 for the join
 template <int D>
 constexpr int few_lds(int nt, int waves) { return waves * (few_patch<D>(nt) + 16 * nt * 8); }
-// Wavefronts of a workgroup that has a compute unit to itself, as many as LDS and registers hold: where there are few rows and heads
-// in all, a tile of tokens takes 1.6 us, whatever runs beside it (one sequence of 512 tokens 13.1 us with 4, 9.0 with 16).
-constexpr int few_waves_alone(int D, int NT) { return D * NT <= 128 ? 16 : D * NT <= 256 ? 8 : 4; }
-constexpr int few_waves_per_simd(int D, int NT) { return D * NT <= 128 ? 4 : D * NT <= 256 ? 2 : 1; }
+// Wavefronts of a workgroup that has a compute unit to itself.  A tile of tokens takes about 1.6 us there whatever runs beside it (its
+// steps wait for one another, more than for memory: tiles fetched two or three ahead change nothing), so more wavefronts are gone
+// through sooner, up to what joining them costs: one sequence of 512 | 1024 tokens 13.1 | 20.0 us with four, 11.7 | 16.4 with eight,
+// 13.1 | 17.3 with sixteen.
+constexpr int few_waves_per_simd(int D, int NT) { return D * NT <= 128 ? 4 : D * NT <= 256 ? 2 : 1; }   // of workgroups that share
+constexpr int few_waves_alone(int D, int NT) { return D * NT <= 256 ? 8 : 4; }
 
 // NT tiles of 16 rows; TERMS: bf16 terms of P
 template <int D, int MODE, int NT, int TERMS, int WAVES>
-__global__ void __launch_bounds__(64 * WAVES, few_waves_per_simd(D, NT)) attn_few_kernel(const AttnArgs a) {
+__global__ void __launch_bounds__(64 * WAVES, WAVES == kWaves ? few_waves_per_simd(D, NT) : WAVES / 4) attn_few_kernel(const AttnArgs a) {
+  // A lane's block is, for D >= 128, what the first product wants of its token from it, if its channels are taken in that order: keys
+  // of plain MXFP4 need no LDS (64 sequences of 8192 tokens, 8 heads: 109 -> 102 us).  Those of a + format do better by it: the block
+  // maximum costs 30 vector instructions in registers and one store there (126 us, and 131 in registers).
+  constexpr bool KEYS_IN_REGISTERS = D >= 128 && MODE == 0;
   constexpr int DB = D / 32, NB = D / 64, PATCH = few_patch<D>(NT);   // blocks per token; per lane of a 32-token tile
   constexpr int LANE_TOKENS = D == 64 ? 32 : 16;             // tokens that a wavefront's lanes cover with one block each (of 2, 4, 4 neighbours)
   extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
@@ -557,7 +581,7 @@ __global__ void __launch_bounds__(64 * WAVES, few_waves_per_simd(D, NT)) attn_fe
     Span span;
     if (!walk.next(a, s, ROWS, kFewUnit, share, r0, span)) continue;
     const int R = s.n * a.group, kv_head = walk.kv_head, part = walk.part;
-    // this lane's rows, as operands of the first product: channels 32 st + 8 quarter ... + 7
+    // this lane's rows, as operands of the first product: eight channels per step
     Operand q[NT][DB];
     int first[NT];                                           // what a row sees of the span: from here,
     uint32_t seen[NT];                                       // so many tokens
@@ -567,10 +591,10 @@ __global__ void __launch_bounds__(64 * WAVES, few_waves_per_simd(D, NT)) attn_fe
       const bool there = r < R;
       first[t] = s.first(a, i);
       seen[t] = there ? tokens_from_to(first[t], s.last(a, i), span.end) : 0u;
-      const uint16_t* p = a.q + (s.q0 + (there ? i : 0)) * a.ld_q + (int64_t)(kv_head * a.group + (there ? r - i * a.group : 0)) * D + 8 * quarter;
+      const uint16_t* p = a.q + (s.q0 + (there ? i : 0)) * a.ld_q + (int64_t)(kv_head * a.group + (there ? r - i * a.group : 0)) * D + (KEYS_IN_REGISTERS ? 32 : 8) * quarter;
 #pragma unroll
       for (int st = 0; st < DB; ++st) {
-        const u32x4 x = *reinterpret_cast<const u32x4*>(p + 32 * st);
+        const u32x4 x = *reinterpret_cast<const u32x4*>(p + (KEYS_IN_REGISTERS ? 128 * (st >> 2) + 8 * (st & 3) : 32 * st));
 #pragma unroll
         for (int j = 0; j < 4; ++j) q[t][st].u[j] = there ? x[j] ^ a.flip : 0u;
       }
@@ -617,23 +641,38 @@ __global__ void __launch_bounds__(64 * WAVES, few_waves_per_simd(D, NT)) attn_fe
       const bool h0 = f.held0, h1 = f.held1;
       uint64_t nan[NB];                                      // lanes whose block of V is NaN: zeros here, put in behind the product
       uint64_t any = 0;
-#pragma unroll
-      for (int i = 0; i < NB; ++i) expand<MODE>(f.k[i], false, patch + 2 * D * tokens_on(i), formed_at_use(lane_at) ^ (64u * blocks_on(i)));
-      __builtin_amdgcn_wave_barrier();
       f32x4 sc[NT][2];
-      const uint32_t k_at = formed_at_use(token_at<D>(col) ^ (16u * quarter));
+      if constexpr (KEYS_IN_REGISTERS) {
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
+        for (int t = 0; t < NT; ++t) sc[t][0] = sc[t][1] = f32x4{0, 0, 0, 0};
 #pragma unroll
-        for (int t = 0; t < NT; ++t) sc[t][h] = f32x4{0, 0, 0, 0};
+        for (int i = 0; i < NB; ++i) {
+          Operand k[4];
+          expand(f.k[i], k);
+          const int h = tokens_on(i) >> 4;
 #pragma unroll
-        for (int st = 0; st < DB; ++st) {
-          Operand k;
-          const u32x4 x = *reinterpret_cast<const u32x4*>(patch + 32 * D * h + (k_at ^ (64u * st)));
+          for (int st = 0; st < 4; ++st)
 #pragma unroll
-          for (int j = 0; j < 4; ++j) k.u[j] = x[j];
+            for (int t = 0; t < NT; ++t) sc[t][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[st].v, q[t][blocks_on(i) + st].v, sc[t][h], 0, 0, 0);
+        }
+      } else {
 #pragma unroll
-          for (int t = 0; t < NT; ++t) sc[t][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k.v, q[t][st].v, sc[t][h], 0, 0, 0);
+        for (int i = 0; i < NB; ++i) expand<MODE>(f.k[i], false, patch + 2 * D * tokens_on(i), formed_at_use(lane_at) ^ (64u * blocks_on(i)));
+        __builtin_amdgcn_wave_barrier();
+        const uint32_t k_at = formed_at_use(token_at<D>(col) ^ (16u * quarter));
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+#pragma unroll
+          for (int t = 0; t < NT; ++t) sc[t][h] = f32x4{0, 0, 0, 0};
+#pragma unroll
+          for (int st = 0; st < DB; ++st) {
+            Operand k;
+            const u32x4 x = *reinterpret_cast<const u32x4*>(patch + 32 * D * h + (k_at ^ (64u * st)));
+#pragma unroll
+            for (int j = 0; j < 4; ++j) k.u[j] = x[j];
+#pragma unroll
+            for (int t = 0; t < NT; ++t) sc[t][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k.v, q[t][st].v, sc[t][h], 0, 0, 0);
+          }
         }
       }
       __builtin_amdgcn_wave_barrier();                       // (the reads above come first: LDS serves a wavefront in order)
