@@ -395,7 +395,8 @@ int mxp_cache_read(const void* cache, int64_t n_pages, int64_t page_tokens, int6
  * bf16 terms (all their bits), for bf16 O as one (to 2^-8).  Values below 2^-126 may count as zero.  lse [rows][heads] fp32 may be NULL.
  * kv_len, table and q_start are read on the device only.  max_q and max_kv are the caller's upper bounds on queries and kv_len of a
  * sequence: they choose launch and splitting, larger sequences are computed all the same, more slowly.
- * rows * heads is at most 2^30 (else MXP_ERR_UNSUPPORTED).
+ * rows * heads is at most 2^30 and, where no sequence is split, a call has fewer than 2^24 tiles of rows (at least one per sequence and
+ * key-value head; else MXP_ERR_UNSUPPORTED).
  * O and lse must not overlap anything that is read.
  * workspace: mxp_attention_workspace_bytes(...) of the same arguments (may be 0), scratch for the parts of split sequences, free
  * again after the call's work on `stream`; a smaller one returns MXP_ERR_WORKSPACE. */

@@ -438,6 +438,7 @@ struct Walk {
 // One row of one head from its parts, by a workgroup: every lane the weights of some parts, then D / 4 lanes across a row and
 // 1024 / D parts at a time.
 constexpr int kMostParts = 1024;
+constexpr float kLeftOut = -1.0f;                            // weight of a part that saw nothing (not 0: a NaN of a part too small to count counts)
 struct JoinRoom {
   float weight[kMostParts], top_of[4], sum_of[4];
   __attribute__((aligned(16))) float acc[1024];
@@ -464,9 +465,9 @@ __device__ __forceinline__ void join_row(const AttnArgs& a, JoinRoom& room, int 
   top = fmaxf(fmaxf(room.top_of[0], room.top_of[1]), fmaxf(room.top_of[2], room.top_of[3]));
 #pragma unroll
   for (int k = 0; k < kMostParts / 256; ++k) {
-    const float f = l[k] == 0.0f ? 0.0f : exp2_of(m[k] - zero_if_none(top));   // (0: a part that saw nothing, left out below)
+    const float f = l[k] == 0.0f ? kLeftOut : exp2_of(m[k] - zero_if_none(top));
     room.weight[t + 256 * k] = f;
-    sum += l[k] * f;
+    if (l[k] != 0.0f) sum += l[k] * f;
   }
 #pragma unroll
   for (int x = 32; x >= 1; x >>= 1) sum += __shfl_xor(sum, x);
@@ -484,8 +485,8 @@ __device__ __forceinline__ void join_row(const AttnArgs& a, JoinRoom& room, int 
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
       const int p = p0 + k * groups;
-      const float w = p < parts ? room.weight[p] : 0.0f;
-      if (w != 0.0f) out += x[k] * w;
+      const float w = p < parts ? room.weight[p] : kLeftOut;
+      if (w != kLeftOut) out += x[k] * w;
     }
   }
   *reinterpret_cast<f32x4*>(room.acc + 4 * t) = out;
@@ -517,8 +518,8 @@ __device__ __forceinline__ void join_row_by_wave(const AttnArgs& a, int parts, P
   float top = m;
 #pragma unroll
   for (int i = 32; i >= 1; i >>= 1) top = fmaxf(top, __shfl_xor(top, i));
-  const float f = l == 0.0f ? 0.0f : exp2_of(m - zero_if_none(top));
-  float sum = l * f;
+  const float f = l == 0.0f ? kLeftOut : exp2_of(m - zero_if_none(top));
+  float sum = l == 0.0f ? 0.0f : l * f;
 #pragma unroll
   for (int i = 32; i >= 1; i >>= 1) sum += __shfl_xor(sum, i);
   f32x4 out = {0, 0, 0, 0};
@@ -527,7 +528,7 @@ __device__ __forceinline__ void join_row_by_wave(const AttnArgs& a, int parts, P
     for (int k = 0; k < 4; ++k) {
       const int p = p0 + g + k * groups;
       const float w = __shfl(f, p & 63);
-      if (p < parts && w != 0.0f) out += (p0 == 0 ? x[k] : *reinterpret_cast<const f32x4*>(a.part_o + part_at(p) * a.g.D + d)) * w;
+      if (p < parts && w != kLeftOut) out += (p0 == 0 ? x[k] : *reinterpret_cast<const f32x4*>(a.part_o + part_at(p) * a.g.D + d)) * w;
     }
   }
   for (int i = across; i < 64; i <<= 1)
@@ -1143,7 +1144,7 @@ extern "C" int mxp_attention(const void* Q, int q_dtype, int64_t ld_q, int64_t r
       off4(kv_len) || off4(table) || off4(lse))
     return MXP_ERR_ALIGN;
   const Plan p = plan_for(n_seq, rows, max_q, max_kv, heads, kv_heads, head_dim, causal, window);
-  if (p.wgs > 2147483647LL) return MXP_ERR_UNSUPPORTED;
+  if (p.wgs >= ((int64_t)1 << 24)) return MXP_ERR_UNSUPPORTED;   // (a launch has fewer than 2^32 threads)
   const size_t need = parts_bytes(p, head_dim);
   if (need > 0 && (!workspace || workspace_bytes < need)) return MXP_ERR_WORKSPACE;
   a.q = static_cast<const uint16_t*>(Q);

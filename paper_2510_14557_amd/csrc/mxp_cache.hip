@@ -162,7 +162,7 @@ constexpr int kCacheUnroll = 4;
 bool cache_unroll(int64_t n_wg) { return n_wg >= (int64_t)kNumCU * 8 * kCacheUnroll; }   // a full chip of workgroups with four groups per lane
 unsigned grid_of(int64_t n_wg) {
   const int64_t n = cache_unroll(n_wg) ? (n_wg + kCacheUnroll - 1) / kCacheUnroll : n_wg;
-  return (unsigned)(n < ((int64_t)1 << 24) ? n : ((int64_t)1 << 24));
+  return (unsigned)(n < ((int64_t)1 << 23) ? n : ((int64_t)1 << 23));   // (a launch has fewer than 2^32 threads)
 }
 
 }  // namespace

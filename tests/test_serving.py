@@ -458,6 +458,27 @@ def test_attention_nan_blocks_count_where_they_are_seen(G, n, D):
 
 
 @gpu
+@pytest.mark.parametrize("kv,n", [(3000, 1), (20000, 1), (3000, 40), (5000, 40)])
+def test_attention_nan_values_of_no_weight_count_too(kv, n):
+    """A NaN block among tokens whose weights are all zero in fp32: no part of a split sequence may be passed over."""
+    b = Batch("MXFP4P", 64, 1, 2, 64, [kv], [n], seed=12)
+    b.q[..., 0] = 64.0                                        # its product with channel 0 decides
+    e, s, i = (x.reshape(b.n_pages * 64, 1, -1) for x in b.q3[0])
+    for tokens, x in ((slice(0, kv // 2), -64.0), (slice(kv // 2, kv), 64.0)):
+        slots = b.slots[0][tokens]
+        rows = np.zeros((len(slots), 64), np.float32)
+        rows[:, 0] = x
+        for to, q in zip((e, s, i), oracle.quantize(rows, b.f)):
+            to[slots, 0] = q.reshape(len(slots), -1)
+        b.val[0][slots, 0] = rows
+    b.poison(0, 5, [1], 1)
+    for out in (torch.bfloat16, torch.float32):
+        o, lse = b.call(out_dtype=out)
+        assert o[..., 32:].isnan().all() and not o[..., :32].isnan().any() and lse.isfinite().all()
+        b.check(o, lse)
+
+
+@gpu
 def test_attention_strides_rows_of_no_sequence_and_device_side_lengths():
     """q a slice of a joint projection, out with gaps; rows before the first and behind the last sequence stay as they are."""
     b = Batch("MXFP4P", 32, 2, 3, 64, [50, 120], [4, 30], seed=8)
@@ -530,7 +551,7 @@ def test_refusals_before_anything_is_launched():
     assert attn(lq=1000) == -2 and attn(lo=512) == -2 and attn(lq=1028) == -3 and attn(lo=1028) == -3
     assert [attn(Q=N), attn(kl=N), attn(tb=N), attn(c=N), attn(O=N)] == [-1] * 5
     assert [attn(Q=odd), attn(O=odd), attn(c=odd), attn(qs=odd), attn(kl=odd), attn(tb=odd), attn(lse=odd)] == [-3] * 7
-    assert attn(rows=1 << 28) == -8 and attn(rows=0, Q=N) == 0 and attn(n=0, Q=N) == 0
+    assert attn(rows=1 << 28) == -8 and attn(rows=1 << 24, n=1 << 24, qs=N, mq=1, heads=2) == -8 and attn(rows=0, Q=N) == 0 and attn(n=0, Q=N) == 0
     need = mxp.attention_workspace_bytes(2, 3, 3, 100000, 8, 2, 128)
     assert need > 0 and attn(mk=100000) == -6 and attn(mk=100000, ws=p, wb=need - 1) == -6
     assert mxp.attention_workspace_bytes(0, 3, 3, 100000, 8, 2, 128) == 0 == mxp.attention_workspace_bytes(2, 3, 3, 100000, 7, 2, 128)
