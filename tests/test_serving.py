@@ -214,6 +214,19 @@ def test_cache_of_many_rows(fmt, dt, D, H, n):
 
 
 @gpu
+def test_cache_of_more_tiles_than_a_grid_has():
+    """Tokens behind the 65535th tile of 8 (head_dim 256): the first and the last of them as the dense conversions have them."""
+    n, D = 65535 * 8 + 21, 256
+    x = torch.randn((2, n, 1, D), device="cuda", generator=torch.Generator("cuda").manual_seed(3)).bfloat16()
+    c = mxp.cache_empty(-(-n // 256), 256, 1, D, mxp.MXFP4P)
+    slots = torch.arange(n, device="cuda")
+    mxp.cache_write(c, x[0], x[1], slots)
+    got = mxp.cache_read(c, slots, torch.bfloat16)
+    for g, want in zip(got, x):
+        assert torch.equal(g.view(n, D), mxp.dequantize(mxp.quantize(want.view(n, D), mxp.MXFP4P), mxp.MXFP4P, torch.bfloat16))
+
+
+@gpu
 def test_cache_beyond_32_bit_offsets():
     """Pages above 4 GiB: written, read and attended to as the first ones are."""
     T, H, D, f = 256, 8, 128, mxp.MXFP4P
