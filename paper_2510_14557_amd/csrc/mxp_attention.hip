@@ -791,33 +791,60 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES == kWaves ? few_waves_per_si
   }
 }
 
-// Four values of a row per lane, for at most kFewParts parts: every lane forms the weights by itself.
-constexpr int kFewParts = 4;
-template <class PartAt>
-__device__ __forceinline__ void join_values(const AttnArgs& a, int parts, PartAt part_at, int64_t row, int head, int d) {
-  float m[kFewParts], l[kFewParts], top = -kInf, sum = 0.0f;
-  f32x4 x[kFewParts], out = {0, 0, 0, 0};
+// Four values of a row per lane, for at most P parts: every lane forms the weights by itself.  (The places behind the last part load the
+// first one again: loads under a condition each are not under way together, and the chunks below then take 155 us instead of 148.)
+template <int P>
+struct FewParts {
+  float m[P], l[P];
+  f32x4 x[P];
+  template <class PartAt>
+  __device__ __forceinline__ void load(const AttnArgs& a, int parts, PartAt part_at, int d) {
 #pragma unroll
-  for (int p = 0; p < kFewParts; ++p) {
-    const int64_t at = part_at(p < parts ? p : 0);
-    m[p] = p < parts ? a.part_ml[2 * at] : -kInf;
-    l[p] = p < parts ? a.part_ml[2 * at + 1] : 0.0f;
-    x[p] = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(a.part_o + at * a.g.D + d));
+    for (int p = 0; p < P; ++p) {
+      const int64_t at = part_at(p < parts ? p : 0);
+      m[p] = p < parts ? a.part_ml[2 * at] : -kInf;
+      l[p] = p < parts ? a.part_ml[2 * at + 1] : 0.0f;
+      x[p] = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(a.part_o + at * a.g.D + d));
+    }
   }
+  __device__ __forceinline__ void finish(const AttnArgs& a, int64_t row, int head, int d) const {
+    float top = -kInf, sum = 0.0f;
+    f32x4 out = {0, 0, 0, 0};
 #pragma unroll
-  for (int p = 0; p < kFewParts; ++p) top = fmaxf(top, m[p]);
+    for (int p = 0; p < P; ++p) top = fmaxf(top, m[p]);
 #pragma unroll
-  for (int p = 0; p < kFewParts; ++p) {
-    if (l[p] == 0.0f) continue;
-    const float f = exp2_of(m[p] - zero_if_none(top));
-    sum += l[p] * f;
-    out += x[p] * f;
+    for (int p = 0; p < P; ++p) {
+      if (l[p] == 0.0f) continue;
+      const float f = exp2_of(m[p] - zero_if_none(top));
+      sum += l[p] * f;
+      out += x[p] * f;
+    }
+    store_out(a, row, head, d, sum == 0.0f ? f32x4{0, 0, 0, 0} : out / sum);
+    if (d == 0 && a.lse) a.lse[row * a.heads + head] = lse_of(top, sum);
   }
-  store_out(a, row, head, d, sum == 0.0f ? f32x4{0, 0, 0, 0} : out / sum);
-  if (d == 0 && a.lse) a.lse[row * a.heads + head] = lse_of(top, sum);
+};
+
+// A tile of rows from at most P parts: a lane's four values of ROWS rows, their loads under way together.  (Three chunks of 777
+// queries behind 3000 to 9001 tokens, 294 tiles of 128 rows in 512 shares: 24 us with one row at once and 16 rows per workgroup, 14.7
+// with two and 64; two and 32: 17.2, four and 64: 19.2.  Eleven of up to 559 queries, with five to eight parts where a wavefront took
+// a row before: 83 -> 78 us in all.)
+template <int P, int ROWS>
+__device__ __forceinline__ void join_tile(const AttnArgs& a, const Sequence& s, int kv_head, int r0, int rows, int rows_per_tile, int first, int parts) {
+  const int shift = __builtin_ctz(a.g.D >> 2), d = 4 * ((int)threadIdx.x & ((a.g.D >> 2) - 1)), step = (256 >> shift) * (int)gridDim.y;
+  for (int row = (int)blockIdx.y * (256 >> shift) + ((int)threadIdx.x >> shift); row < rows; row += ROWS * step) {
+    FewParts<P> f[ROWS];
+#pragma unroll
+    for (int u = 0; u < ROWS; ++u)
+      if (row + u * step < rows) f[u].load(a, parts, [&](int p) { return ((int64_t)2 * (first + p) + (p == 0 ? 1 : 0)) * rows_per_tile + row + u * step; }, d);
+#pragma unroll
+    for (int u = 0; u < ROWS; ++u) {
+      const int r = r0 + row + u * step, query = r / a.group;
+      if (row + u * step < rows) f[u].finish(a, s.q0 + query, kv_head * a.group + r - query * a.group, d);
+    }
+  }
 }
 
-// The joins that Share records, `each` workgroups' records per workgroup here, in the one of three ways that fits the parts.
+// The joins that Share records, `each` workgroups' records per workgroup here, in the way that fits the parts: few, up to 64, more.
 __global__ void __launch_bounds__(256) attn_join_kernel(const AttnArgs a, int rows_per_tile, int n_records, int each) {
   __shared__ JoinRoom room;
   const int lane = threadIdx.x & 63, first = (int)blockIdx.x * each;
@@ -827,14 +854,10 @@ __global__ void __launch_bounds__(256) attn_join_kernel(const AttnArgs a, int ro
     const int32_t* const j = a.joins + 4 * g;
     const Sequence s(a, j[0]);
     const int kv_head = j[1], r0 = j[2], parts = j[3] - g + 1, R = s.n * a.group;
-    if (parts <= kFewParts) {
-      const int across = a.g.D >> 2;
-      for (int i = (int)blockIdx.y * 256 + (int)threadIdx.x; i < rows_per_tile * across; i += 256 * (int)gridDim.y) {
-        const int row = i / across, r = r0 + row, query = r / a.group;
-        if (r >= R) break;
-        join_values(a, parts, [&](int p) { return ((int64_t)2 * (g + p) + (p == 0 ? 1 : 0)) * rows_per_tile + row; }, s.q0 + query,
-                    kv_head * a.group + r - query * a.group, 4 * (i - row * across));
-      }
+    if (parts <= 8) {
+      const int rows = R - r0 < rows_per_tile ? R - r0 : rows_per_tile;
+      if (parts <= 4) join_tile<4, 2>(a, s, kv_head, r0, rows, rows_per_tile, g, parts);
+      else join_tile<8, 1>(a, s, kv_head, r0, rows, rows_per_tile, g, parts);
       continue;
     }
     const bool by_wave = parts <= 64;
@@ -1187,13 +1210,13 @@ extern "C" int mxp_attention(const void* Q, int q_dtype, int64_t ld_q, int64_t r
 #undef MXP_ATTN_T
   if (!p.direct) {
     // About so many parts a join: above 32 there are few records, 16 of them and one row per workgroup (one sequence of 131000 tokens,
-    // 8 joins of 128 parts: 14.6 -> 7.8 us against a record each); else a record per workgroup, one row per wavefront or, as a few
-    // parts take them, 16 rows.
+    // 8 joins of 128 parts: 14.6 -> 7.8 us against a record each); else a record per workgroup, one row per wavefront or, where
+    // joins have about as few parts as join_tile takes (twice the average in the longest sequences), 64 rows.
     const int64_t parts_each = p.wgs / (n_seq * kv_heads * p.row_tiles);
     int64_t most = (max_q < rows ? max_q : rows) * a.group;
     most = most < 1 ? 1 : most < p.rows ? most : p.rows;
     const int each = parts_each >= 32 ? 16 : 1;
-    const int64_t y = parts_each >= 32 ? most : parts_each >= kFewParts ? (most + 3) / 4 : (most + 15) / 16;
+    const int64_t y = parts_each >= 32 ? most : parts_each >= 4 ? (most + 3) / 4 : (most + 63) / 64;
     hipLaunchKernelGGL(attn_join_kernel, dim3((unsigned)((p.wgs + each - 1) / each), (unsigned)y), dim3(256), 0, s, a, p.rows,
                        (int)p.wgs, each);
   }
