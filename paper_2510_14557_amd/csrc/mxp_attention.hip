@@ -16,8 +16,8 @@
 // 8192 tokens, 8 heads of 128, 32 query heads, MXFP4+: 90 us = 4.2 TB/s with the join's 5 us; of 8192 each 4.8, plain MXFP4 5.6; the
 // loads alone 78 us of the 90; vector ALU 66 %, LDS 60 %, matrix cores 12 % of the time).
 // attn_many_kernel: 128 rows per workgroup, the wavefronts share the de-converted tokens; bound by the softmax's vector instructions and
-// the matrix cores in turn (one prompt of 8192 tokens, 32 heads of 128 on 8: 627 us = 877 TFLOP/s; vector ALU 55 %, matrix cores 37 %,
-// LDS 33 %; the next tile's scores formed among this one's weights: 648 us, the registers do not hold both).
+// the matrix cores in turn (one prompt of 8192 tokens, 32 heads of 128 on 8: 608 us = 905 TFLOP/s; vector ALU 55 %, matrix cores 37 %,
+// LDS 33 %; the next tile's scores formed among this one's weights: 3 % slower, the registers do not hold both).
 // Both can deal a sequence's tokens out to several workgroups; attn_join_kernel then joins the parts.
 #include "mxp_cache.h"
 
@@ -55,7 +55,7 @@ struct AttnArgs {
   int o_bf16;
   float *lse, *part_o, *part_ml;                             // parts of rows: D values, maximum and sum
   int32_t* joins;                                            // few rows: [workgroup][4], see Share
-  int direct, row_tiles;
+  int row_tiles;
 };
 
 constexpr int kWaves = 4;                                     // of a workgroup
@@ -368,13 +368,15 @@ __device__ __forceinline__ void find_share(const AttnArgs& a, int rows, int unit
   __syncthreads();
 }
 
-// The rows and tokens that a workgroup goes over, one run after another: its share, or (a.direct) whole tiles of rows.
+// The rows and tokens that a workgroup goes over, one run after another: its share, or (DIRECT) whole tiles of rows.  Two kernels, not a
+// branch in one: with the code of both, a prompt of 500 tokens took 24.0 us instead of 21.6, one of 8192 tokens 627 instead of 608.
+template <bool DIRECT>
 struct Walk {
   int seq, kv_head = 0, tile = 0, item = 0, off = 0, me = 0;
   int64_t left = 0, end = 0;
   int part = -1;                                             // where a run's result goes: out, or among the parts
   __device__ __forceinline__ Walk(const AttnArgs& a, int rows, int unit, int least, bool near, Share& share, int64_t (&wave_sum)[kWaves]) {
-    if (a.direct) {
+    if constexpr (DIRECT) {
       // key-value head fastest (consecutive workgroups go to different XCDs: with 8 heads an XCD's cache has one to hold), then tile
       // of rows, the longest first, then sequence
       uint32_t id = blockIdx.x;
@@ -394,13 +396,13 @@ struct Walk {
     }
   }
   // whether there is more to do; `seq` is a sequence's number only then
-  __device__ __forceinline__ bool more(const AttnArgs& a) const { return a.direct || (left > 0 && seq < a.n_seq); }
-  __device__ __forceinline__ bool more(const AttnArgs& a, const Sequence& s, int rows) const { return !a.direct || tile * rows < s.n * a.group; }
+  __device__ __forceinline__ bool more(const AttnArgs& a) const { return DIRECT || (left > 0 && seq < a.n_seq); }
+  __device__ __forceinline__ bool more(const AttnArgs& a, const Sequence& s, int rows) const { return !DIRECT || tile * rows < s.n * a.group; }
   // The next run: its tile of rows and span of tokens.  False where the sequence has none left (the next one may).
   __device__ __forceinline__ bool next(const AttnArgs& a, const Sequence& s, int rows, int unit, const Share& share, int& r0, Span& span) {
     const int R = s.n * a.group;
     int from = 0, to = 0x7FFFFFFF;
-    if (a.direct) {
+    if constexpr (DIRECT) {
       const int tiles = (R + rows - 1) / rows;
       r0 = (tiles - 1 - tile) * rows;                        // the last rows see most: they start first
       tile += a.row_tiles;
@@ -557,7 +559,7 @@ constexpr int few_waves_per_simd(int D, int NT) { return D * NT <= 128 ? 4 : D *
 constexpr int few_waves_alone(int D, int NT) { return D * NT <= 256 ? 8 : 4; }
 
 // NT tiles of 16 rows; TERMS: bf16 terms of P
-template <int D, int MODE, int NT, int TERMS, int WAVES>
+template <int D, int MODE, int NT, int TERMS, int WAVES, bool DIRECT>
 __global__ void __launch_bounds__(64 * WAVES, WAVES == kWaves ? few_waves_per_simd(D, NT) : WAVES / 4) attn_few_kernel(const AttnArgs a) {
   // A lane's block is, for D >= 128, what the first product wants of its token from it, if its channels are taken in that order: keys
   // of plain MXFP4 need no LDS (64 sequences of 8192 tokens, 8 heads: 109 -> 102 us).  Those of a + format do better by it: the block
@@ -578,7 +580,7 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES == kWaves ? few_waves_per_si
   constexpr int ROWS = 16 * NT;
   __shared__ Share share;
   __shared__ int64_t wave_sum[kWaves];
-  for (Walk walk(a, ROWS, kFewUnit, kFewLeast, false, share, wave_sum);;) {
+  for (Walk<DIRECT> walk(a, ROWS, kFewUnit, kFewLeast, false, share, wave_sum);;) {
     if (!walk.more(a)) break;
     const Sequence s(a, walk.seq);
     if (!walk.more(a, s, ROWS)) break;
@@ -878,7 +880,7 @@ constexpr int many_jobs() { return 2 * kManyTokens * (D / 32) / (64 * kWaves); }
 template <int D>
 constexpr int many_lds() { return 2 * 2 * kManyTokens * 2 * D + 2 * kWaves * many_jobs<D>() * 8; }   // two buffers of keys and values; NaN masks
 
-template <int D, int MODE, int TERMS>
+template <int D, int MODE, int TERMS, bool DIRECT>
 __global__ void __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) attn_many_kernel(const AttnArgs a) {
   constexpr int DB = D / 32, HALF = kManyTokens * 2 * D, JOBS = many_jobs<D>();
   extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
@@ -892,7 +894,7 @@ __global__ void __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) attn_many_kerne
   const auto job_block = [&](int k, int who) { return D == 64 ? who >> 5 : 4 * (k >> 1) + (who >> 4); };
   __shared__ Share share;
   __shared__ int64_t wave_sum[kWaves];
-  for (Walk walk(a, kManyRows, kManyTokens, kManyLeast, true, share, wave_sum);;) {
+  for (Walk<DIRECT> walk(a, kManyRows, kManyTokens, kManyLeast, true, share, wave_sum);;) {
     if (!walk.more(a)) break;
     const Sequence s(a, walk.seq);
     if (!walk.more(a, s, kManyRows)) break;
@@ -1110,24 +1112,30 @@ Plan plan_for(int64_t n_seq, int64_t rows, int64_t max_q, int64_t max_kv, int64_
 int64_t part_rows(const Plan& p) { return p.direct ? 0 : p.wgs * 2 * p.rows; }
 size_t parts_bytes(const Plan& p, int64_t D) { return p.direct ? 0 : (size_t)part_rows(p) * (size_t)(D + 2) * 4 + (size_t)p.wgs * 16; }
 
-template <int D, int MODE, int NT, int TERMS, int WAVES>
+template <int D, int MODE, int NT, int TERMS, int WAVES, bool DIRECT>
 void launch_few(const AttnArgs& a, const Plan& p, hipStream_t s) {
   constexpr int bytes = few_lds<D>(NT, WAVES);
-  allow_dynamic_lds<attn_few_kernel<D, MODE, NT, TERMS, WAVES>>(bytes);
-  hipLaunchKernelGGL((attn_few_kernel<D, MODE, NT, TERMS, WAVES>), dim3((unsigned)p.wgs), dim3(64 * WAVES), bytes, s, a);
+  allow_dynamic_lds<attn_few_kernel<D, MODE, NT, TERMS, WAVES, DIRECT>>(bytes);
+  hipLaunchKernelGGL((attn_few_kernel<D, MODE, NT, TERMS, WAVES, DIRECT>), dim3((unsigned)p.wgs), dim3(64 * WAVES), bytes, s, a);
 }
 template <int D, int MODE, int NT, int TERMS>
 void launch_few(const AttnArgs& a, const Plan& p, hipStream_t s) {
-  if (p.alone) launch_few<D, MODE, NT, TERMS, few_waves_alone(D, NT)>(a, p, s);
-  else launch_few<D, MODE, NT, TERMS, kWaves>(a, p, s);
+  if (p.alone) launch_few<D, MODE, NT, TERMS, few_waves_alone(D, NT), true>(a, p, s);
+  else if (p.direct) launch_few<D, MODE, NT, TERMS, kWaves, true>(a, p, s);
+  else launch_few<D, MODE, NT, TERMS, kWaves, false>(a, p, s);
+}
+
+template <int D, int MODE, int TERMS, bool DIRECT>
+void launch_many(const AttnArgs& a, const Plan& p, hipStream_t s) {
+  allow_dynamic_lds<attn_many_kernel<D, MODE, TERMS, DIRECT>>(many_lds<D>());
+  hipLaunchKernelGGL((attn_many_kernel<D, MODE, TERMS, DIRECT>), dim3((unsigned)p.wgs), dim3(64 * kWaves), many_lds<D>(), s, a);
 }
 
 template <int D, int MODE, int TERMS>
 void launch(const AttnArgs& a, const Plan& p, hipStream_t s) {
-  const dim3 grid((unsigned)p.wgs);
   if (p.many) {
-    allow_dynamic_lds<attn_many_kernel<D, MODE, TERMS>>(many_lds<D>());
-    hipLaunchKernelGGL((attn_many_kernel<D, MODE, TERMS>), grid, dim3(64 * kWaves), many_lds<D>(), s, a);
+    if (p.direct) launch_many<D, MODE, TERMS, true>(a, p, s);
+    else launch_many<D, MODE, TERMS, false>(a, p, s);
   } else if (p.rows == 32) {
     launch_few<D, MODE, 2, TERMS>(a, p, s);
   } else {
@@ -1198,7 +1206,6 @@ extern "C" int mxp_attention(const void* Q, int q_dtype, int64_t ld_q, int64_t r
   const size_t parts = (size_t)part_rows(p);
   a.part_ml = need ? a.part_o + parts * head_dim : nullptr;
   a.joins = need ? reinterpret_cast<int32_t*>(a.part_ml + 2 * parts) : nullptr;
-  a.direct = p.direct ? 1 : 0;
   a.row_tiles = p.row_tiles;
   hipStream_t s = static_cast<hipStream_t>(stream);
 #define MXP_ATTN_T(D, M) do { if (a.o_bf16) launch<D, M, 1>(a, p, s); else launch<D, M, 3>(a, p, s); } while (0)

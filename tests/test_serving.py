@@ -383,6 +383,20 @@ def test_attention_ragged_queries(out, fmt, D, T, H, G, window):
 
 
 @gpu
+@pytest.mark.parametrize("out", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("fmt", FOUR)
+@pytest.mark.parametrize("D", [64, 128, 256])
+def test_attention_both_launches_of_many_rows(out, fmt, D):
+    """Many rows behind long contexts, dealt out in shares; the same tokens without their contexts, whole tiles of rows."""
+    b = Batch(fmt, 64, 2, 2, D, [2600, 1300], [70, 45], seed=31)
+    assert mxp.attention_workspace_bytes(2, 115, 70, 2600, 4, 2, D) > 0
+    b.check(*b.call(out_dtype=out))
+    b = Batch(fmt, 64, 2, 2, D, [70, 45], [70, 45], seed=32)
+    assert mxp.attention_workspace_bytes(2, 115, 70, 70, 4, 2, D) == 0
+    b.check(*b.call(out_dtype=out))
+
+
+@gpu
 @pytest.mark.parametrize("nq", [[1, 1], [6, 40]])
 def test_attention_not_causal_and_other_scales(nq):
     b = Batch("MXFP4P", 16, 2, 4, 128, [77, 200], nq, seed=3)
