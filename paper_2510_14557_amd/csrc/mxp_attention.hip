@@ -16,8 +16,8 @@
 // 8192 tokens, 8 heads of 128, 32 query heads, MXFP4+: 90 us = 4.2 TB/s with the join's 5 us; of 8192 each 4.8, plain MXFP4 5.6; the
 // loads alone 78 us of the 90; vector ALU 66 %, LDS 60 %, matrix cores 12 % of the time).
 // attn_many_kernel: 128 rows per workgroup, the wavefronts share the de-converted tokens; bound by the softmax's vector instructions and
-// the matrix cores in turn (one prompt of 8192 tokens, 32 heads of 128 on 8: 608 us = 905 TFLOP/s; vector ALU 55 %, matrix cores 37 %,
-// LDS 33 %; the next tile's scores formed among this one's weights: 3 % slower, the registers do not hold both).
+// the matrix cores in turn (one prompt of 8192 tokens, 32 heads of 128 on 8: 608 us = 905 TFLOP/s; vector ALU 57 %, matrix cores 39 %,
+// LDS 35 %; the next tile's scores formed among this one's weights: 3 % slower, the registers do not hold both).
 // Both can deal a sequence's tokens out to several workgroups; attn_join_kernel then joins the parts.
 #include "mxp_cache.h"
 
