@@ -146,12 +146,14 @@ struct Sequence {
   }
 };
 
-// The tokens [begin, end) that any of `rows` > 0 rows from `row` on sees, begin a multiple of 32
+// The tokens [first, end) that any of `rows` > 0 rows from `row` on sees (each of them by some row); begin: where the tiles of tokens
+// start, a multiple of 32 at most 31 tokens in front of them, or a share's begin.
 struct Span {
-  int begin = 0, end = 0;
+  int first = 0, begin = 0, end = 0;
   Span() = default;
   __device__ __forceinline__ Span(const AttnArgs& a, const Sequence& s, int row, int rows) {
-    begin = s.first(a, row / a.group) & ~31;
+    first = s.first(a, row / a.group);
+    begin = first & ~31;
     end = s.last(a, (row + rows - 1) / a.group) + 1;
   }
 };
@@ -183,6 +185,10 @@ struct Page {
 struct Block {
   u32x4 code;
   uint32_t scale, index;
+  // To be expanded to zeros, as a flushed block is.  For values in front of the first token that any row sees: their slots may never have
+  // been written, and weights of 0 do not hide an Inf or NaN.  Only the first tile of a span has such tokens, so they are blanked once,
+  // ahead of the loop (tested inside it, the one number more that lives through the loop spills: 64 sequences 89 -> 95 us).
+  __device__ __forceinline__ void blank() { scale = index = 0u; }
 };
 
 // ONCE: no other workgroup of the call reads these codes (64 sequences of 2048 to 8192 tokens 98.6 -> 93.5 us with streaming loads)
@@ -754,6 +760,11 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES == kWaves ? few_waves_per_si
     };
 #pragma unroll
     for (int u = 0; u < kFewAhead; ++u) fetch(ahead[u], begin + u * 32 * WAVES);
+    if (begin < span.first && begin < span.end) {
+#pragma unroll
+      for (int i = 0; i < NB; ++i)
+        if (begin + lane_token + tokens_on(i) < span.first) ahead[0].v[i].blank();
+    }
     for (int t0 = begin; t0 < span.end; t0 += kFewAhead * 32 * WAVES)
 #pragma unroll
       for (int u = 0; u < kFewAhead; ++u) take(ahead[u], t0 + u * 32 * WAVES);
@@ -966,6 +977,11 @@ __global__ void __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) attn_many_kerne
     int buf = 0;
     if (span.begin < span.end) {
       fetch(span.begin);
+      if (span.begin < span.first) {
+#pragma unroll
+        for (int k = 0; k < JOBS; ++k)
+          if (job_of_v(k) && span.begin + job_token(wave, lane) < span.first) job[k].blank();
+      }
       expand_all(span.begin, 0);
     }
     for (int t0 = span.begin; t0 < span.end; t0 += kManyTokens) {

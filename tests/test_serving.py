@@ -506,6 +506,29 @@ def test_attention_nan_values_of_no_weight_count_too(kv, n):
 
 
 @gpu
+@pytest.mark.parametrize("out", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("fmt", FOUR)
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("kv,nq,window", [([150, 33, 77], [1, 1, 1], 40), ([150, 64], [5, 5], 45), ([300, 130], [60, 20], 45), ([5000, 900], [2, 2], 3000),
+                                          ([4100], [70], 2500)])
+def test_attention_slots_in_front_of_a_window_may_hold_anything(out, fmt, D, kv, nq, window):
+    """Slots that nobody sees, before a window and behind the last token, hold bytes that no conversion leaves: scale bytes 253 to 255,
+    scales below their delta.  Few and many rows, whole tiles and shares."""
+    b = Batch(fmt, 16, 2, 2, D, kv, nq, seed=16)
+    if window > 1000:
+        assert mxp.attention_workspace_bytes(len(kv), int(b.start[-1]), max(nq), max(kv), 4, 2, D, window=window) > 0
+    unseen = np.ones(b.n_pages * 16, bool)
+    for n, m, slots in zip(kv, nq, b.slots):
+        unseen[slots[max(n - m - window + 1, 0):]] = False
+    assert sum(unseen[slots].sum() for slots in b.slots) > 0
+    rng = np.random.default_rng(17)
+    for e, s, i in (tuple(x.reshape(b.n_pages * 16, 2, -1) for x in q) for q in b.q3):
+        for x, values in ((e, range(256)), (s, (1, 2, 253, 254, 255)), (i, range(256))):
+            x[unseen] = rng.choice(values, x[unseen].shape)
+    b.check(*b.call(out_dtype=out, window=window), window=window)
+
+
+@gpu
 def test_attention_strides_rows_of_no_sequence_and_device_side_lengths():
     """q a slice of a joint projection, out with gaps; rows before the first and behind the last sequence stay as they are."""
     b = Batch("MXFP4P", 32, 2, 3, 64, [50, 120], [4, 30], seed=8)
