@@ -389,7 +389,8 @@ int mxp_cache_read(const void* cache, int64_t n_pages, int64_t page_tokens, int6
  * causal: query i of n sees token t <= kv_len - n + i (the last query sees all); with window > 0 (causal only) also
  * t > kv_len - n + i - window.  Not causal: every t < kv_len.  A page number outside [0, n_pages) stands for tokens that nobody sees.
  * A row that sees nothing gets O = 0 and lse = -infinity.  What an invisible token's slot holds, a NaN block included, has no
- * influence; a visible NaN block makes the scores (keys) or the 32 outputs (values) it meets NaN.
+ * influence; a visible NaN block (scale byte 255, whatever its index byte) makes the scores (keys) or the 32 outputs (values) it meets
+ * NaN.  A visible token's slot must otherwise hold what a conversion writes: scale bytes up to 252, in MXFP4++ above their delta (or 0).
  * Q is MXP_BF16 (MXP_F32: MXP_ERR_UNSUPPORTED); keys and values are de-converted by Eq. 2 (exact) inside the kernel and multiplied
  * on the bf16 MFMA; scores, softmax and sums are fp32.  For fp32 O the weights p enter the second product as three
  * bf16 terms (all their bits), for bf16 O as one (to 2^-8).  Values below 2^-126 may count as zero.  lse [rows][heads] fp32 may be NULL.

@@ -223,13 +223,14 @@ __device__ __forceinline__ uint32_t formed_at_use(uint32_t at) {
 }
 
 // A block's 32 bf16 into LDS, its first byte at tile + at (`at` as above, with the block's channels).  A flushed block, or one to be
-// left out (`drop`), becomes zeros; a scale byte of 255 makes the unpack-converts answer NaN (also for zero codes, so what is left
-// out gets another).
+// left out (`drop`), becomes zeros; a scale byte of 255 makes the unpack-converts answer NaN, also for zero codes, so what is left out
+// gets another.  Both go by the scale byte, whatever the index byte says (an NBM scale below 0 counts as 0).
 template <int MODE>
 __device__ __forceinline__ void expand(const Block& b, bool drop, uint8_t* tile, uint32_t at) {
   const bool zero = drop || b.scale == 0u;
   const uint32_t keep = zero ? 0u : 0xFFFFFFFFu;
-  const float X = __uint_as_float((drop ? 127u : b.scale - (MODE == 2 ? b.index >> 5 : 0u)) << 23);
+  const uint32_t delta = MODE == 2 && b.scale != 255u ? b.index >> 5 : 0u;
+  const float X = __uint_as_float((drop ? 127u : __builtin_elementwise_sub_sat(b.scale, delta)) << 23);
 #pragma unroll
   for (uint32_t j = 0; j < 4; ++j) {
     const uint32_t c = b.code[j] & keep;

@@ -529,6 +529,24 @@ def test_attention_slots_in_front_of_a_window_may_hold_anything(out, fmt, D, kv,
 
 
 @gpu
+@pytest.mark.parametrize("fmt", FOUR)
+@pytest.mark.parametrize("n", [1, 10, 40])
+@pytest.mark.parametrize("D", [64, 128, 256])
+def test_attention_nan_and_zero_blocks_whatever_their_index_bytes(fmt, n, D):
+    """A scale byte of 255 is NaN and one of 0 zeros, in keys and values, also with a position and a delta left in the index byte."""
+    b = Batch(fmt, 16, 2, 2, D, [150, 95, 40], [n] * 3, seed=18)
+    for seq, t, block, part, index in ((0, 149, 0, 0, 0xE9), (1, 94, D // 32 - 1, 1, 0xE9), (2, 39, 0, 0, 0x29), (2, 38, D // 32 - 1, 1, 0x29)):
+        b.poison(seq, t, [block], part)
+        b.q3[part][2].reshape(b.n_pages * 16, 2, -1)[b.slots[seq][t], :, block] = index
+        if seq == 2:
+            b.q3[part][1].reshape(b.n_pages * 16, 2, -1)[b.slots[2][t], :, block] = 0
+            b.val[part][b.slots[2][t], :, 32 * block:32 * block + 32] = 0
+    o, lse = b.call(out_dtype=torch.float32)
+    assert o[n - 1].isnan().all() and lse[n - 1].isnan().all() and not o[2 * n:].isnan().any()
+    b.check(o, lse)
+
+
+@gpu
 def test_attention_strides_rows_of_no_sequence_and_device_side_lengths():
     """q a slice of a joint projection, out with gaps; rows before the first and behind the last sequence stay as they are."""
     b = Batch("MXFP4P", 32, 2, 3, 64, [50, 120], [4, 30], seed=8)
