@@ -46,7 +46,7 @@ struct AttnArgs {
   const int32_t *q_start, *kv_len, *table;
   int64_t ld_table;
   int n_seq, heads, group, causal, window;                   // group: query heads per key-value head; window 0: none
-  float scale;                                               // |scale| * log2(e), at least the smallest normal number
+  float scale, up;                                           // |scale| * log2(e), at least the smallest normal number; kGrowth over it
   uint32_t flip;                                             // sign bits of two bf16 where scale is negative: Q is negated
   const uint8_t* data;
   CacheGeom g;
@@ -60,9 +60,11 @@ struct AttnArgs {
 
 constexpr int kWaves = 4;                                     // of a workgroup
 constexpr float kInf = __builtin_inff();
-// The reference of a row's weights follows its running maximum only where that is more than 2^kGrowth ahead: a weight is then at
-// most 2^kGrowth instead of 1, with the same relative error in bf16 and in the fp32 sums, and most tiles of tokens need no rescaling.
-constexpr float kGrowth = 8.0f;
+// What a row's weights refer to, m, is set 2^kGrowth above the largest score seen, and again only where a score exceeds it: most tiles of
+// tokens need no rescaling, and a weight is never above 1, so that sums of weighted values stay below those of the values.  Weights
+// of 2^-kGrowth have the relative error of larger ones in bf16 and in the fp32 sums; below 2^-118 of the row's largest they may count as 0.
+constexpr float kGrowth = 8.0f, kMostFloat = 3.40282347e38f;
+__device__ __forceinline__ float raised(float m, float mx, float up) { return mx > m ? fminf(mx + up, kMostFloat) : m; }
 __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ float zero_if_none(float m) { return m == -kInf ? 0.0f : m; }   // 2^(x - m) where nothing was seen yet
 
@@ -716,7 +718,8 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES == kWaves ? few_waves_per_si
       for (int t = 0; t < NT; ++t) {
         float mx = fmaxf(fmaxf(fmaxf(sc[t][0][0], sc[t][0][1]), fmaxf(sc[t][0][2], sc[t][0][3])), fmaxf(fmaxf(sc[t][1][0], sc[t][1][1]), fmaxf(sc[t][1][2], sc[t][1][3])));
         mx = fmaxf(m[t], max_across_32(max_across_16(mx)));
-        if (__any((mx - m[t]) * a.scale > kGrowth)) {
+        if (__any(mx > m[t])) {
+          mx = raised(m[t], mx, a.up);
           const float fade = exp2_of((m[t] - zero_if_none(mx)) * a.scale);
           l[t] *= fade;
 #pragma unroll
@@ -1027,7 +1030,8 @@ __global__ void __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) attn_many_kerne
 #pragma unroll
           for (int j = 0; j < 16; ++j) mx = fmaxf(mx, sc[h][j]);
         mx = fmaxf(m, max_across_32(mx));
-        if (__any((mx - m) * a.scale > kGrowth)) {
+        if (__any(mx > m)) {
+          mx = raised(m, mx, a.up);
           const float fade = exp2_of((m - zero_if_none(mx)) * a.scale);
           l *= fade;
 #pragma unroll
@@ -1213,6 +1217,7 @@ extern "C" int mxp_attention(const void* Q, int q_dtype, int64_t ld_q, int64_t r
   a.window = (int)(window < 2147483647LL ? window : 2147483647LL);
   a.scale = (scale < 0 ? -scale : scale) * 1.4426950408889634f;
   if (a.scale < 1.17549435e-38f) a.scale = 1.17549435e-38f;   // (0 would make NaN of a hidden token's -infinity)
+  a.up = kGrowth / a.scale < 8.5e37f ? kGrowth / a.scale : 8.5e37f;   // (a number: -infinity stays where nothing was seen)
   a.flip = scale < 0 ? 0x80008000u : 0u;
   a.data = static_cast<const uint8_t*>(cache);
   a.o = O;

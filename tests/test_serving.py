@@ -547,6 +547,31 @@ def test_attention_nan_and_zero_blocks_whatever_their_index_bytes(fmt, n, D):
 
 
 @gpu
+@pytest.mark.parametrize("out", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("n", [1, 12, 40])
+@pytest.mark.parametrize("period,max_kv", [(128, 1100), (256, 1)])
+def test_attention_large_values_behind_a_lagging_maximum(out, D, n, period, max_kv):
+    """Values up to 2^117, scores that rise by 2^7 (base 2) without the weights being rescaled: sum p |v| with p <= 1 stays below
+    1024 * 2^117, so nothing overflows on the way to a finite result."""
+    b = Batch("MXFP4P", 64, 1, 2, D, [1024], [n], seed=19)
+    assert (mxp.attention_workspace_bytes(1, n, n, max_kv, 2, 1, D) > 0) == (max_kv > 1)
+    b.q.zero_()
+    b.q[..., 0] = 4.84375                                     # * 4 * 0.25 * log2(e) = 6.99
+    rows = np.zeros((2, 1024, D), np.float32)
+    rows[0, np.arange(1024) // period % 2 == 1, 0] = 4.0
+    rows[1] = 2.0 ** 116 * (1 + 0.99 * np.random.default_rng(20).random((1024, D)))
+    for part in (0, 1):
+        q = oracle.quantize(rows[part], b.f)
+        for to, x in zip(b.q3[part], q):
+            to.reshape(b.n_pages * 64, -1)[b.slots[0]] = x
+        b.val[part][b.slots[0], 0] = oracle.dequantize(q, b.f)
+    o, lse = b.call(out_dtype=out, scale=0.25, max_kv=max_kv)
+    assert o.isfinite().all()
+    b.check(o, lse, scale=0.25)
+
+
+@gpu
 def test_attention_strides_rows_of_no_sequence_and_device_side_lengths():
     """q a slice of a joint projection, out with gaps; rows before the first and behind the last sequence stay as they are."""
     b = Batch("MXFP4P", 32, 2, 3, 64, [50, 120], [4, 30], seed=8)
