@@ -394,7 +394,8 @@ int mxp_cache_read(const void* cache, int64_t n_pages, int64_t page_tokens, int6
  * Q is MXP_BF16 (MXP_F32: MXP_ERR_UNSUPPORTED); keys and values are de-converted by Eq. 2 (exact) inside the kernel and multiplied
  * on the bf16 MFMA; scores, softmax and sums are fp32.  For fp32 O the weights p enter the second product as three
  * bf16 terms (all their bits), for bf16 O as one (to 2^-8).  Values below 2^-126 may count as zero, and so may weights 2^-118 below a
- * row's largest.  The sums of weighted values are fp32 numbers, with weights of at most 1: they cannot overflow for values below
+ * row's largest.  A row whose largest scale * q . k lies beyond fp32 comes out NaN; a score of -infinity (an infinite value of Q) counts
+ * as not seen.  The sums of weighted values are fp32 numbers, with weights of at most 1: they cannot overflow for values below
  * 2^127 / kv_len.  lse [rows][heads] fp32 may be NULL.
  * kv_len, table and q_start are read on the device only.  max_q and max_kv are the caller's upper bounds on queries and kv_len of a
  * sequence: they choose launch and splitting, larger sequences are computed all the same, more slowly.

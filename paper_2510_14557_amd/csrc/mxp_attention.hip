@@ -1077,6 +1077,7 @@ __global__ void __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) attn_many_kerne
       }
     }
     l = sum_across_32(l);
+    if (m * a.scale == kInf) l = __builtin_nanf("");         // (scores beyond fp32, all weights 0: not a row that sees nothing)
     if (there) {
       const int64_t part_row = part < 0 ? -1 : (int64_t)part * kManyRows + 32 * wave + col;
 #pragma unroll

@@ -572,6 +572,22 @@ def test_attention_large_values_behind_a_lagging_maximum(out, D, n, period, max_
 
 
 @gpu
+@pytest.mark.parametrize("out", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("kv", [200, 3000])
+@pytest.mark.parametrize("n", [1, 12, 40])
+def test_attention_scores_beyond_fp32_are_not_taken_for_nothing_seen(out, kv, n):
+    """Products of scale and score above 2^128: NaN in O and lse; the rows of zero scores beside them are averages of the values."""
+    b = Batch("MXFP4P", 16, 1, 2, 64, [kv], [n], seed=21)
+    b.q[:, 0] = 0
+    o, lse = b.call(out_dtype=out, scale=2e38)
+    assert o[:, 1].isnan().all() and lse[:, 1].isnan().all()
+    b.q[:, 1] = 0
+    both, both_lse = b.call(out_dtype=out)
+    both[:, 0], both_lse[:, 0] = o[:, 0], lse[:, 0]
+    b.check(both, both_lse)
+
+
+@gpu
 def test_attention_strides_rows_of_no_sequence_and_device_side_lengths():
     """q a slice of a joint projection, out with gaps; rows before the first and behind the last sequence stay as they are."""
     b = Batch("MXFP4P", 32, 2, 3, 64, [50, 120], [4, 30], seed=8)
