@@ -588,6 +588,33 @@ def test_attention_scores_beyond_fp32_are_not_taken_for_nothing_seen(out, kv, n)
 
 
 @gpu
+@pytest.mark.parametrize("T,D,kv,n,max_kv,splits", [
+    (16, 64, [9000], 1, 1, False), (16, 128, [9000], 1, 1, False),               # eight wavefronts: 8192 tokens per lookup
+    (16, 64, [9000] + [20] * 260, 1, 1, False), (32, 256, [9000], 10, 1, False),  # four: 4096
+    (16, 64, [20000], 1, 600, True), (16, 128, [20000], 3, 600, True),           # the same in shares
+    (16, 64, [2500], 40, 1, False), (16, 128, [2500, 1100], 40, 1, False), (16, 256, [2500], 20, 1, False),   # many rows: 1024
+    (16, 64, [9000], 40, 1100, True), (16, 128, [9000], 40, 1100, True)])
+def test_attention_looks_pages_up_again(T, D, kv, n, max_kv, splits):
+    """Runs of tokens longer than the page numbers that a wavefront holds at once; a bound on kv_len below the truth makes them so long."""
+    H, G = 1, 3 if n == 10 else 2
+    b = Batch("MXFP4P", T, H, G, D, kv, [n] * len(kv), seed=24)
+    assert (mxp.attention_workspace_bytes(len(kv), n * len(kv), n, max_kv, H * G, H, D) > 0) == splits
+    for out in (torch.bfloat16, torch.float32):
+        b.check(*b.call(out_dtype=out, max_kv=max_kv))
+
+
+@gpu
+@pytest.mark.parametrize("D,kv,n,least", [(64, 140000, 1, 257), (128, 20000, 1, 65), (256, 20000, 2, 65)])
+def test_attention_joins_of_many_parts(D, kv, n, least):
+    """One sequence and one key-value head in more than 64 and more than 256 parts."""
+    b = Batch("MXFP4P", 64, 1, 4, D, [kv], [n], seed=25)
+    # a share leaves room for two parts of 16 rows: D values, maximum and sum; and its record
+    assert mxp.attention_workspace_bytes(1, n, n, kv, 4, 1, D) >= least * (2 * 16 * (D + 2) * 4 + 16)
+    for out in (torch.bfloat16, torch.float32):
+        b.check(*b.call(out_dtype=out))
+
+
+@gpu
 def test_attention_strides_rows_of_no_sequence_and_device_side_lengths():
     """q a slice of a joint projection, out with gaps; rows before the first and behind the last sequence stay as they are."""
     b = Batch("MXFP4P", 32, 2, 3, 64, [50, 120], [4, 30], seed=8)
