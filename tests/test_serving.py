@@ -856,6 +856,108 @@ def test_a_layer_captured_and_replayed(own_stream):
         torch.randn(1000, device="cuda").sum().item()
 
 
+class LongLayer(Layer):
+    """A layer with room for thousands of tokens, so that attention is dealt out in shares and joined, and a product behind it."""
+
+    def __init__(self):
+        super().__init__(pages=256)
+        gen = torch.Generator(device="cuda").manual_seed(1)
+        assert mxp.attention_workspace_bytes(self.n, self.n, 1, 256 * self.T, self.G * self.H, self.H, self.D) > 0
+        self.qo = mxp.quantize((torch.randn((256, self.G * self.H * self.D), generator=gen, device="cuda") * 0.06).bfloat16(), mxp.MXFP4P)
+        self.past = [torch.randn((256 * self.T, self.n * self.H, self.D), generator=gen, device="cuda").bfloat16() for _ in range(2)]
+
+    def begin(self, lengths):
+        """Contexts of these lengths, written by an eager prefill; the layer's step then goes on from there."""
+        for s, n in enumerate(lengths):
+            t = torch.arange(n, device="cuda")
+            mxp.cache_write(self.cache, *(p[:n, s * self.H:(s + 1) * self.H] for p in self.past), self.table[s, t // self.T].long() * self.T + t % self.T)
+        self.kv_len.copy_(torch.tensor(lengths, dtype=torch.int32))
+
+    def step(self):
+        super().step()
+        self.y = mxp.gemm(mxp.quantize(self.o.view(self.n, -1), mxp.MXFP8), mxp.MXFP8, self.qo, mxp.MXFP4P, torch.bfloat16)
+
+    def results(self):
+        return self.h, self.qkv, self.o, self.y, self.kv_len
+
+    def expected(self):
+        """The attention in 64 bits on the cache's tokens, and how far an output may be off: Batch.check's bound for bf16."""
+        outs = []
+        for s, n in enumerate(self.kv_len.tolist()):
+            t = torch.arange(n, device="cuda")
+            k, v = (x.double().cpu().numpy().repeat(self.G, 1) for x in mxp.cache_read(self.cache, self.table[s, t // self.T].long() * self.T + t % self.T, torch.float32))
+            q = self.qkv[s, :self.H * self.G].double().cpu().numpy()
+            z = np.einsum("hd,thd->ht", q, k) * self.D ** -0.5
+            p = np.exp(z - z.max(-1, keepdims=True))
+            p /= p.sum(-1, keepdims=True)
+            o, S = np.einsum("ht,thd->hd", p, v), np.einsum("ht,thd->hd", p, abs(v))
+            size = np.einsum("hd,thd->ht", abs(q), abs(k)).max() * self.D ** -0.5
+            outs.append((o, (4 * (self.D + 8) * 2.0 ** -24 * size + 2.0 ** -8 + (n + 64) * 2.0 ** -24) * S + 2.0 ** -8 * abs(o)))
+        return (np.stack(x) for x in zip(*outs))
+
+
+LENGTHS = ([0, 0, 0], [1, 3000, 0], [4000, 4090, 2222], [5, 6, 7], [0, 4095, 130])   # before a step; shares without work among them
+
+
+@gpu
+@pytest.mark.parametrize("own_stream", [False, True])
+def test_a_layer_with_split_sequences_captured_and_replayed(own_stream):
+    """The parts' workspace and the joins in a HIP graph: replays at lengths set from outside, each against the eager step and 64 bits."""
+    L, E = LongLayer(), LongLayer()
+    L.step(); E.step()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        L.step()
+    side = torch.cuda.Stream()
+    for turn, lengths in enumerate(LENGTHS * 2):
+        new = torch.randn(L.x.shape, generator=torch.Generator().manual_seed(turn)).bfloat16().cuda()
+        for layer in (L, E):
+            layer.x.copy_(new)
+            layer.begin(lengths)
+        L.ws.fill_(255)                                       # nothing is kept in the workspace from call to call
+        graph.replay()
+        if own_stream:
+            side.wait_stream(torch.cuda.current_stream())
+            with torch.cuda.stream(side):
+                E.step()
+            torch.cuda.current_stream().wait_stream(side)
+        else:
+            E.step()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(L.results(), E.results()))
+        o, tol = L.expected()
+        assert (abs(L.o.double().cpu().numpy() - o) <= tol).all()
+
+
+@gpu
+def test_two_layers_on_two_streams():
+    """Whole layers, attention dealt out in shares, on two streams at once: as one after the other."""
+    layers = [LongLayer(), LongLayer()]
+    for i, layer in enumerate(layers):
+        layer.x.mul_(i + 1)
+    want = []
+    for lengths in LENGTHS:
+        for layer in layers:
+            layer.begin(lengths)
+            layer.step()
+            want.append([x.clone() for x in layer.results()])
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in layers]
+    got = [[], []]
+    for layer, stream, out in zip(layers, streams, got):
+        stream.wait_stream(torch.cuda.current_stream())
+    for lengths in LENGTHS:
+        for layer, stream, out in zip(layers, streams, got):
+            with torch.cuda.stream(stream):
+                layer.begin(lengths)
+                layer.step()
+                out.append([x.clone() for x in layer.results()])
+    torch.cuda.synchronize()
+    for i in range(2):
+        for a, b in zip(got[i], want[i::2]):
+            assert all(torch.equal(x, y) for x, y in zip(a, b))
+
+
 @gpu
 def test_two_streams_with_workspaces_of_their_own():
     """Split sequences on two streams at once: each call's parts lie in its own workspace."""
