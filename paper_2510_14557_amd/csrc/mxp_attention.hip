@@ -13,11 +13,13 @@
 //
 // Query rows of one key-value head (heads that share it x queries) are taken together.  attn_few_kernel: up to 32 of them per
 // workgroup, every wavefront with tokens of its own, joined through LDS at the end; bound by reading the cache (64 sequences of 2048 to
-// 8192 tokens, 8 heads of 128, 32 query heads, MXFP4+: 90 us = 4.2 TB/s with the join's 5 us; of 8192 each 4.8, plain MXFP4 5.6; the
-// loads alone 78 us of the 90; vector ALU 66 %, LDS 60 %, matrix cores 12 % of the time).
+// 8192 tokens, 8 heads of 128, 32 query heads, MXFP4+: 90 us = 4.2 TB/s with the join's 5 us; of 8192 each 4.7, plain MXFP4 5.2, with
+// 64 query heads and pages of 64 5.5; the loads alone 78 us of the 90; vector ALU 66 %, LDS 60 %, matrix cores 12 % of the time).
 // attn_many_kernel: 128 rows per workgroup, the wavefronts share the de-converted tokens; bound by the softmax's vector instructions and
-// the matrix cores in turn (one prompt of 8192 tokens, 32 heads of 128 on 8: 608 us = 905 TFLOP/s; vector ALU 57 %, matrix cores 39 %,
-// LDS 35 %; the next tile's scores formed among this one's weights: 3 % slower, the registers do not hold both).
+// the matrix cores in turn (one prompt of 8192 tokens, 32 heads of 128 on 8: 600 to 627 us on several machines = 877 to 916 TFLOP/s;
+// vector ALU 56 %, matrix cores 39 %, LDS 35 %; the next tile's scores formed among this one's weights: 3 % slower, the registers do
+// not hold both).  At head_dim 256 the registers do not hold a wavefront's rows either: 31 to 52 a lane lie in scratch memory (a prompt
+// of 2048 tokens 193 us = 356 TFLOP/s).
 // Both can deal a sequence's tokens out to several workgroups; attn_join_kernel then joins the parts.
 #include "mxp_cache.h"
 
@@ -93,8 +95,10 @@ __device__ __forceinline__ uint32_t bf16_pair(float a, float b) {   // rounded t
 
 constexpr int64_t kMostTokens = (int64_t)1 << 30, kMostRows = (int64_t)1 << 30;   // per sequence; rows x heads of a call
 
-// Eight weights of one row, 2^(scale x - base), as the bf16 terms of an operand; their sum.  A term is the rounded rest that the
-// terms before it leave: three hold all 24 bits.
+// Eight weights of one row, 2^(scale x - base), as the bf16 terms of an operand; their sum, of the unrounded ones.  A term is the
+// rounded rest that the terms before it leave: three hold all 24 bits, for fp32 results.  bf16 results have one: their relative error
+// against 64 bits (norms) is then 2.1e-3 to 2.3e-3, of which the rounding of the results alone is 1.65e-3.  Two terms leave that only, at
+// another product per tile of V: the prompt 605 -> 762 us, 64 sequences of one query 89.5 -> 94.
 template <int TERMS>
 __device__ __forceinline__ float weights(f32x4 x0, f32x4 x1, float scale, float base, Operand (&p)[TERMS]) {
   float e[8], sum = 0.0f;
@@ -193,7 +197,7 @@ struct Block {
   __device__ __forceinline__ void blank() { scale = index = 0u; }
 };
 
-// ONCE: no other workgroup of the call reads these codes (64 sequences of 2048 to 8192 tokens 98.6 -> 93.5 us with streaming loads)
+// ONCE: no other workgroup of the call reads these codes (64 sequences of 2048 to 8192 tokens 95.5 -> 89.4 us with streaming loads)
 template <int D, int MODE, bool ONCE>
 __device__ __forceinline__ Block load_block(const uint8_t* rec, const CacheGeom& g, int row, int blk) {
   Block b;
@@ -218,7 +222,7 @@ __device__ __forceinline__ uint32_t token_at(int token) {
 }
 
 // A place whose variants (^ b) are to be formed where they are used: kept in registers over the loop, they cost the few-row kernel its
-// fourth wavefront per SIMD (64 sequences of 8192 tokens: 151 us, and 135 so).
+// fourth wavefront per SIMD or spill (64 sequences of 2048 to 8192 tokens: 95.2 us, and 89.4 so; of plain MXFP4, 8192 each: 114, and 109).
 __device__ __forceinline__ uint32_t formed_at_use(uint32_t at) {
   asm volatile("" : "+v"(at));
   return at;
@@ -317,7 +321,7 @@ struct Load {
   }
 };
 // Shares of so many units, each at least `least`, or half of that while they are fewer than the compute units (one sequence of 2048
-// tokens, 8 heads: 19.0 us with four, 15.8 with two; 16 such sequences 24 with four, 29 with two).
+// tokens, 8 heads: 17.0 us with four, 14.8 with two; 16 such sequences 22.3 with four, 26.1 with two).
 __host__ __device__ inline int64_t shares_of(int64_t units, int64_t least) {
   const int64_t n = (units + least - 1) / least, twice = (units + least / 2 - 1) / (least / 2);
   return n >= kNumCU ? n : twice < kNumCU ? twice : kNumCU;
@@ -352,7 +356,7 @@ __device__ __forceinline__ void find_share(const AttnArgs& a, int rows, int unit
   }
   const int64_t most = shares_of(total, least), n = most < (int64_t)gridDim.x ? most : (int64_t)gridDim.x;
   // near: neighbouring shares, which then often read the same tokens, on one XCD (workgroups go to the eight of them in turn).  Chunks
-  // behind long contexts 187 -> 184 us; few rows, whose tokens nobody else reads, lose 3 % by it.
+  // behind long contexts 151.8 -> 148.4 us; few rows, whose tokens nobody else reads, gain nothing by it.
   const int64_t eights = near ? n >> 3 : 0, id = blockIdx.x, g = id < 8 * eights ? (id & 7) * eights + (id >> 3) : id;
   if (threadIdx.x == 0) share.me = (int)g;
   if (g < n) {
@@ -562,8 +566,11 @@ template <int D>
 constexpr int few_lds(int nt, int waves) { return waves * (few_patch<D>(nt) + 16 * nt * 8); }
 // Wavefronts of a workgroup that has a compute unit to itself.  A tile of tokens takes about 1.6 us there whatever runs beside it (its
 // steps wait for one another, more than for memory: tiles fetched two or three ahead change nothing), so more wavefronts are gone
-// through sooner, up to what joining them costs: one sequence of 512 | 1024 tokens 13.1 | 20.0 us with four, 11.7 | 16.4 with eight,
-// 13.1 | 17.3 with sixteen.
+// through sooner, up to what joining them costs: one sequence of 512 | 1024 | 2048 tokens 11.5 | 18.2 | 29.3 us with four, 10.7 | 15.3 |
+// 22.2 with eight, 12.4 | 16.7 | 22.0 with sixteen.
+// The registers that this leaves do not suffice for 32 rows of head_dim 256, where 25 to 42 a lane lie in scratch memory (64 sequences of
+// 2048 to 8192 tokens, 32 query heads on 8: one query 189 us, five 484; at head_dim 128 90 and 127), nor, in workgroups that share,
+// for 32 rows of head_dim 64 with fp32 results (9 to 17).
 constexpr int few_waves_per_simd(int D, int NT) { return D * NT <= 128 ? 4 : D * NT <= 256 ? 2 : 1; }   // of workgroups that share
 constexpr int few_waves_alone(int D, int NT) { return D * NT <= 256 ? 8 : 4; }
 
@@ -571,8 +578,8 @@ constexpr int few_waves_alone(int D, int NT) { return D * NT <= 256 ? 8 : 4; }
 template <int D, int MODE, int NT, int TERMS, int WAVES, bool DIRECT>
 __global__ void __launch_bounds__(64 * WAVES, WAVES == kWaves ? few_waves_per_simd(D, NT) : WAVES / 4) attn_few_kernel(const AttnArgs a) {
   // A lane's block is, for D >= 128, what the first product wants of its token from it, if its channels are taken in that order: keys
-  // of plain MXFP4 need no LDS (64 sequences of 8192 tokens, 8 heads: 109 -> 102 us).  Those of a + format do better by it: the block
-  // maximum costs 30 vector instructions in registers and one store there (126 us, and 131 in registers).
+  // of plain MXFP4 need no LDS (64 sequences of 8192 tokens, 8 heads: 115.6 -> 109.0 us).  Those of a + format do better by it: the block
+  // maximum costs 30 vector instructions in registers and one store there (4 % slower in registers).
   constexpr bool KEYS_IN_REGISTERS = D >= 128 && MODE == 0;
   constexpr int DB = D / 32, NB = D / 64, PATCH = few_patch<D>(NT);   // blocks per token; per lane of a 32-token tile
   constexpr int LANE_TOKENS = D == 64 ? 32 : 16;             // tokens that a wavefront's lanes cover with one block each (of 2, 4, 4 neighbours)
@@ -1099,8 +1106,11 @@ struct Plan {
 };
 
 // Sequences of at most so many tokens are not dealt out in parts: a workgroup goes over them in less than the parts' join takes.
-// (Few rows, us whole | dealt out: 8 tiles of rows of 1024 tokens 17.1 | 15.9, of 2048 22.7 | 15.8; 128 of 1024 17.5 | 19.4, of 2048
-// 23.8 | 29; 320 of 2048 40 | 44.)
+// (Few rows, us whole | dealt out, tiles of rows of 1024 tokens, of 2048, head_dim 128: 8 tiles 14.3 | 14.0, 22.2 | 15.1; 32: 15.0 | 14.6,
+// 22.4 | 15.5; 64: 15.4 | 14.8, 22.8 | 18.2; 80: 15.6 | 20.0, 22.9 | 21.6; 128: 15.7 | 18.1, 23.2 | 22.3; 320: 23.6 | 26.2, 38.5 | 41.5;
+// MXFP4++ the same within 0.4 us, of 1024 tokens at 8 tiles 15.5 | 14.7.  At head_dim 256 whole tiles are behind at more tiles too:
+// 8: 25.9 | 19.4, 38.8 | 20.2; 64: 26.6 | 20.3, 41.7 | 26.6; 80: 26.8 | 28.2, 41.8 | 33.0; 128: 27.2 | 26.4, 42.4 | 34.7; 320: 43.1 | 44.9,
+// 71.5 | 65.1; the rule does not heed it.)
 constexpr int64_t kFewDirect = 2048, kFewestDirect = 512, kManyDirect = 1024;
 
 // Which kernel (up to 32 rows of a key-value head: attn_few_kernel), and whether a workgroup takes whole tiles of rows or a share of
