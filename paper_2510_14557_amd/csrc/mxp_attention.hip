@@ -1227,7 +1227,8 @@ extern "C" int mxp_attention(const void* Q, int q_dtype, int64_t ld_q, int64_t r
   a.causal = causal ? 1 : 0;
   a.window = (int)(window < 2147483647LL ? window : 2147483647LL);
   a.scale = (scale < 0 ? -scale : scale) * 1.4426950408889634f;
-  if (a.scale < 1.17549435e-38f) a.scale = 1.17549435e-38f;   // (0 would make NaN of a hidden token's -infinity)
+  if (a.scale < 1.17549435e-38f) a.scale = 1.17549435e-38f;   // (0 would make NaN of a hidden token's -infinity,
+  if (a.scale > kMostFloat) a.scale = kMostFloat;             // infinity of a score of 0)
   a.up = kGrowth / a.scale < 8.5e37f ? kGrowth / a.scale : 8.5e37f;   // (a number: -infinity stays where nothing was seen)
   a.flip = scale < 0 ? 0x80008000u : 0u;
   a.data = static_cast<const uint8_t*>(cache);

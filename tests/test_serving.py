@@ -615,6 +615,16 @@ def test_attention_joins_of_many_parts(D, kv, n, least):
 
 
 @gpu
+@pytest.mark.parametrize("n", [1, 12, 40])
+def test_attention_of_zero_scores_whatever_the_scale(n):
+    """Any finite scale is taken, also one whose product with log2(e) is not: 0 times it is 0, and O the average of the values."""
+    b = Batch("MXFP4P", 16, 1, 2, 64, [200], [n], seed=26)
+    b.q.zero_()
+    for scale in (3.4e38, -3.4e38, 1e-45):
+        b.check(*b.call(out_dtype=torch.float32, scale=scale))
+
+
+@gpu
 def test_attention_strides_rows_of_no_sequence_and_device_side_lengths():
     """q a slice of a joint projection, out with gaps; rows before the first and behind the last sequence stay as they are."""
     b = Batch("MXFP4P", 32, 2, 3, 64, [50, 120], [4, 30], seed=8)
