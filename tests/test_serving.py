@@ -130,6 +130,21 @@ def test_norm_in_place_strided_and_rows_of_nothing():
         assert e.shape[0] == shape[0] and e.numel() == 0
 
 
+@gpu
+@pytest.mark.parametrize("K", [64, 1056, 16416])
+def test_norm_of_more_rows_than_a_grid_has(K):
+    """Rows behind the 16384 workgroups of a launch, of one wavefront, of several and in two passes: as calls of 1000 rows have them."""
+    n = 2 * 16384 + 333 if K < 16000 else 16384 + 333
+    gen = torch.Generator(device="cuda").manual_seed(K)
+    x, r = (torch.randn((n, K), generator=gen, device="cuda").bfloat16() for _ in range(2))
+    w = torch.randn(K, generator=gen, device="cuda")
+    q, h = mxp.rmsnorm_quantize(x, w, mxp.MXFP8P, residual=r)
+    for at in (0, 16000, 16384, n - 1000):
+        rows = slice(at, at + 1000)
+        part, hp = mxp.rmsnorm_quantize(x[rows], w, mxp.MXFP8P, residual=r[rows])
+        assert torch.equal(h[rows], hp) and all(torch.equal(a[rows], b) for a, b in zip(q, part))
+
+
 # ---- the cache ------------------------------------------------------------------------------------------------------
 def records(e, s, i, n_pages, T, H, D, fmt):
     """Oracle bytes of rows [page][token][head] as the cache's records [page][head][bytes]."""
