@@ -1,7 +1,7 @@
 // mxp_attention: softmax attention of ragged query rows over the paged four-bit cache (layout: mxp_cache.h).
 //
 // One pass over the visible tokens with the running maximum and sum of the softmax, in base 2 (the scale carries log2 e):
-//     S = K Q^T     m' = max(m, S)     P = 2^(S - m')     l = l 2^(m - m') + sum P     O = O 2^(m - m') + V^T P
+//     S = K Q^T     m' = max(m, S)     P = 2^(S - m')     l = l 2^(m - m') + sum P     O = O 2^(m - m') + V^T P     (m: see kGrowth)
 // Both products have the tokens' side as their first operand, so the result of the first, [token][row], has a query row per lane
 // column and four or sixteen tokens in a lane's registers: what the second takes as its second operand, up to a permutation of the
 // tokens inside one MFMA step, which the reads of V follow.  Maximum, sum and rescaling are then a lane's own business (plus one
@@ -55,7 +55,7 @@ struct AttnArgs {
   void* o;
   int64_t ld_o;
   int o_bf16;
-  float *lse, *part_o, *part_ml;                             // parts of rows: D values, maximum and sum
+  float *lse, *part_o, *part_ml;                             // parts of rows: D values; what their weights refer to, their sum
   int32_t* joins;                                            // few rows: [workgroup][4], see Share
   int row_tiles;
 };
